@@ -44,7 +44,8 @@ typedef enum {
     NT_ERR_DEVICE = 5            /* HIP runtime error (launch failure, no device) */
 } nt_status;
 
-typedef enum { NT_F16 = 0, NT_BF16 = 1, NT_F32 = 2 } nt_dtype;
+/* NT_E4M3 (8-bit floating point, 4 exponent and 3 mantissa bits, no infinities) and NT_I8: codes of a paged cache only. */
+typedef enum { NT_F16 = 0, NT_BF16 = 1, NT_F32 = 2, NT_E4M3 = 3, NT_I8 = 4 } nt_dtype;
 
 /* A source tensor: sizes and element strides, as a framework front end reports them
  * (Section 3.2.1, last paragraph). */
@@ -322,6 +323,70 @@ nt_status nt_matmul_views(const void *A, const nt_tensor_desc *dA, const nt_meta
 nt_status nt_sdpa(const void *q, const nt_tensor_desc *dq, const void *k, const nt_tensor_desc *dk,
                   const void *v, const nt_tensor_desc *dv, void *o, const nt_tensor_desc *dout,
                   float scale, nt_dtype dtype, void *hip_stream);
+
+/* ---------------------------------------------------------------- paged key / value cache (device)
+ *
+ * The past of many sequences in pages of a fixed number of tokens.  K and V are device tensors [pages, page_size, heads,
+ * head_size] (descriptors of ndim 4, equal sizes; any strides along the first three axes, so a cache stored [pages, heads, page_size,
+ * head_size] is a permuted descriptor; unit stride along the last; head_size a multiple of 8 up to 256).  Slot s is place s % page_size of
+ * page s / page_size.  dtype is the tokens' type (NT_F16 or NT_BF16), or NT_E4M3 / NT_I8: then each token's head is held as codes
+ * and a scale of its own, fp32 device tensors [pages, page_size, heads] (any strides), its value being code * scale.
+ * A 16-bit cache has no scales (NULL).
+ */
+typedef struct {
+    void *k, *v;
+    const nt_tensor_desc *dk, *dv;
+    float *k_scale, *v_scale;
+    const nt_tensor_desc *dks, *dvs;
+    nt_dtype dtype;
+} nt_paged_cache;
+
+/* nt_cache_write: puts token t's K and V ([tokens, heads, head_size], elements of `dtype`, unit stride along the last axis) into slot
+ * slots[t] (a DEVICE array of int64, one per token).  A slot outside the cache (negative: padding) is passed over.  The slots of one
+ * call must differ: of tokens that share one, each element may be any one's.  16-bit caches hold the elements as they are; 8-bit ones
+ *   scale = max |x| / L over the token's head, L = 448 (NT_E4M3) or 127 (NT_I8), rounded up to twelve significant bits and at least 2^-100
+ *           (NT_F16: at most 146.1875 or 515.75, the largest of twelve bits that keeps L * scale in the type's range),
+ *   code  = x / scale rounded to the nearest code, ties to the even one
+ * (the real quotient decides).  A head with an infinity or NaN gets the scale NaN and codes 0: all of it reads as NaN.
+ */
+nt_status nt_cache_write(const nt_paged_cache *cache, const void *k, const nt_tensor_desc *dk, const void *v, const nt_tensor_desc *dv,
+                         const int64_t *slots, nt_dtype dtype, void *hip_stream);
+
+/* nt_cache_read: the inverse: K and V of slot slots[t] to row t of k and v, codes times scales rounded once to `dtype`.  Slots may repeat;
+ * one outside the cache gives zeros. */
+nt_status nt_cache_read(const nt_paged_cache *cache, void *k, const nt_tensor_desc *dk, void *v, const nt_tensor_desc *dv,
+                        const int64_t *slots, nt_dtype dtype, void *hip_stream);
+
+/* nt_sdpa_paged: attention of new tokens over a paged cache that holds them and what was before them.
+ * Sequence b has the new tokens starts[b] .. starts[b + 1] - 1 of q and out ([tokens, query heads, head_size], elements of `dtype`, unit stride
+ * along the last axis; the query heads a multiple of the cache's heads: query head h reads cache head h / (query heads / heads)), and
+ * lengths[b] tokens in the cache, the new ones last: new token i of n is at position p = lengths[b] - n + i.  Position j lies on page
+ * table[b][j / page_size].  table: device int32 [sequences, entries], unit stride along the entries; starts (sequences + 1 entries, not
+ * decreasing) and lengths: device int32 arrays.
+ *   out[t,h,:] = sum_j softmax_j(scale <q[t,h,:], K_j>) V_j  over the positions 0 <= j < lengths[b] that the token sees:
+ *   j <= p if `causal`, and j > p - window if window > 0.
+ * What a token does not see has no part in its result, whatever it holds.  A token that sees nothing (a length below the new tokens' count, or 0), or
+ * nothing with a score above -inf, gets zeros.  A token that sees a position whose page the table does not name (an entry outside the
+ * cache, such as -1, or a position past the table's last entry) gets NaN.  Rows of q that belong to no sequence are passed over.  scale = 0
+ * stands for 1 / sqrt(head_size).  out must not alias an input.
+ * Scores, weights' sums and accumulators are fp32, the weights are rounded to `dtype` before they multiply V; 8-bit codes are exact in
+ * either type, K's scale multiplies the score and V's the weight, in fp32.
+ * max_queries, max_length: the most new tokens and the greatest length of a sequence, if the host knows them (0: it does not); they choose the
+ * kernel and how the keys are shared out, so a bound that is too low costs time, not results.
+ * Memory: the keys of long sequences are shared out over programs where there are few of them; the shares pass through the library's
+ * workspace under the rules given at nt_conv2d_implicit, and are added in a fixed order.
+ */
+nt_status nt_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_paged_cache *cache, const int32_t *table, const nt_tensor_desc *d_table,
+                        const int32_t *starts, const int32_t *lengths, void *out, const nt_tensor_desc *dout,
+                        float scale, int32_t causal, int64_t window, int64_t max_queries, int64_t max_length, nt_dtype dtype, void *hip_stream);
+
+/* How the calling thread's last nt_sdpa_paged call was laid out; zeros if nothing was launched.  For tests and diagnostics. */
+typedef struct {
+    int32_t rows;            /* (token, query head) rows per program: 16 or 32 (wavefronts share the keys), or 128 (they share the rows) */
+    int32_t shares;          /* programs that a row's keys are shared out over */
+    int32_t share_keys;      /* keys of one share (0: not shared) */
+} nt_paged_plan;
+nt_status nt_last_paged_plan(nt_paged_plan *out);
 
 /* nt_bmm: the same per batch index; descriptors have ndim 3: [batch,M,K], [batch,K,N], [batch,M,N]
  * (listed among the paper's kernels in Section 5.1). */

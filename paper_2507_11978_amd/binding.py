@@ -50,6 +50,17 @@ class SdpaPlan(C.Structure):
     _fields_ = [("queries", C.c_int32), ("groups", C.c_int32), ("wavefronts", C.c_int32), ("matrix_sums", C.c_int32), ("streamed", C.c_int32)]
 
 
+class PagedCache(C.Structure):
+    """A paged key / value cache (see nt_paged_cache)."""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("dk", C.POINTER(TensorDesc)), ("dv", C.POINTER(TensorDesc)),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("dks", C.POINTER(TensorDesc)), ("dvs", C.POINTER(TensorDesc)), ("dtype", C.c_int32)]
+
+
+class PagedPlan(C.Structure):
+    """How the last attention call over a paged cache was laid out (see nt_paged_plan)."""
+    _fields_ = [("rows", C.c_int32), ("shares", C.c_int32), ("share_keys", C.c_int32)]
+
+
 _lib = None
 
 
@@ -125,6 +136,10 @@ def load():
     L.nt_conv2d_implicit.argtypes = [P, D, P, D, P, D, i32, i32, i32, i32, i32, i32, TileCfg, P]
     L.nt_matmul_views.argtypes = [P, D, O, i32, P, D, O, i32, P, D, O, i32, i32, i32, TileCfg, P]
     L.nt_sdpa.argtypes = [P, D, P, D, P, D, P, D, C.c_float, i32, P]
+    PC = C.POINTER(PagedCache)
+    L.nt_cache_write.argtypes = [PC, P, D, P, D, P, i32, P]
+    L.nt_cache_read.argtypes = [PC, P, D, P, D, P, i32, P]
+    L.nt_sdpa_paged.argtypes = [P, D, PC, P, D, P, P, P, D, C.c_float, i32, i64, i64, i64, i32, P]
     L.nt_add.argtypes = [P, D, P, D, P, D, i32, i64, P]
     L.nt_silu.argtypes = [P, D, P, D, i32, i64, P]
     L.nt_softmax.argtypes = [P, D, P, D, i32, P]
@@ -134,7 +149,8 @@ def load():
     L.nt_trace_loader_slice.argtypes = [i32, P, D, P, D, D, i32, i32, i32, i32, i32, i32, TileCfg, i32, i64, i64, P, C.c_size_t, P]
     for name in ("nt_arrange_levels", "nt_arrange_tile", "nt_arrange_gemm", "nt_arrange_bmm", "nt_arrange_conv2d",
                  "nt_program_order", "nt_gemm", "nt_gemm_noalloc", "nt_addmm", "nt_addmm_act", "nt_bmm", "nt_conv2d_implicit", "nt_trace_tile", "nt_trace_loader_slice",
-                 "nt_add", "nt_silu", "nt_softmax", "nt_rms_norm", "nt_matmul_views", "nt_sdpa", "nt_mfma_probe"):
+                 "nt_add", "nt_silu", "nt_softmax", "nt_rms_norm", "nt_matmul_views", "nt_sdpa", "nt_cache_write", "nt_cache_read",
+                 "nt_sdpa_paged", "nt_mfma_probe"):
         getattr(L, name).restype = i32
     L.nt_last_kernel_path.restype = i32
     L.nt_last_k_split.restype = i32
@@ -142,6 +158,8 @@ def load():
     L.nt_last_conv_plan.restype = i32
     L.nt_last_sdpa_plan.argtypes = [C.POINTER(SdpaPlan)]
     L.nt_last_sdpa_plan.restype = i32
+    L.nt_last_paged_plan.argtypes = [C.POINTER(PagedPlan)]
+    L.nt_last_paged_plan.restype = i32
     L.nt_last_error.restype = C.c_char_p
     L.nt_version.restype = C.c_char_p
     _lib = L
@@ -176,7 +194,8 @@ def _load_calls():
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
         module.bind(*(C.cast(getattr(lib, name), C.c_void_p).value
-                      for name in ("nt_gemm", "nt_bmm", "nt_addmm", "nt_addmm_act", "nt_conv2d_implicit", "nt_sdpa", "nt_softmax", "nt_rms_norm", "nt_add", "nt_silu")))
+                      for name in ("nt_gemm", "nt_bmm", "nt_addmm", "nt_addmm_act", "nt_conv2d_implicit", "nt_sdpa", "nt_softmax", "nt_rms_norm", "nt_add", "nt_silu",
+                                   "nt_cache_write", "nt_cache_read", "nt_sdpa_paged")))
     except (ImportError, OSError) as e:                     # not built, or built for another torch
         module = _calls = _Declining()
         warnings.warn(f"{_CALLS_PATH} cannot be loaded ({e}): calls are marshalled through ctypes, some 2 us slower each; "
@@ -443,6 +462,13 @@ def last_sdpa_plan() -> SdpaPlan:
     return plan
 
 
+def last_paged_plan() -> PagedPlan:
+    """How the calling thread's last sdpa_paged() was laid out."""
+    plan = PagedPlan()
+    _check(load().nt_last_paged_plan(C.byref(plan)))
+    return plan
+
+
 ACTIVATIONS = {None: 0, "none": 0, "relu": 1, "silu": 2, "gelu_tanh": 3}
 
 
@@ -567,6 +593,104 @@ def sdpa(q, k, v, out, scale=0.0, stream=None):
     _require_cuda(q, k, v, out)
     _check(load().nt_sdpa(q.data_ptr(), _ref(q), k.data_ptr(), _ref(k), v.data_ptr(), _ref(v),
                           out.data_ptr(), _ref(out), float(scale), _code(q), _stream_ptr(stream)))
+    return out
+
+
+_cache_codes: dict = {}
+
+
+def _cache(k_cache, v_cache, k_scale, v_scale):
+    """The C description of a paged cache (a reference to it keeps it, and the descriptors it names, alive)."""
+    import torch
+    if not _cache_codes:
+        _cache_codes.update({torch.float16: _DTYPES["f16"], torch.bfloat16: _DTYPES["bf16"], torch.float8_e4m3fn: 3, torch.int8: 4})
+    if (k_scale is None) != (v_scale is None):
+        raise ValueError("scales of both K and V, or of neither")
+    _require_cuda(k_cache, v_cache, *(() if k_scale is None else (k_scale, v_scale)))
+    if k_cache.dtype not in _cache_codes or v_cache.dtype != k_cache.dtype:
+        raise ValueError("K and V caches must share one of the types float16, bfloat16, float8_e4m3fn and int8")
+    descs = [make_desc(t.shape, t.stride()) for t in (k_cache, v_cache)]
+    c = PagedCache(k_cache.data_ptr(), v_cache.data_ptr(), C.pointer(descs[0]), C.pointer(descs[1]), None, None, None, None, _cache_codes[k_cache.dtype])
+    if k_scale is not None:
+        if k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32:
+            raise ValueError("scales must be float32")
+        descs += [make_desc(t.shape, t.stride()) for t in (k_scale, v_scale)]
+        c.k_scale, c.v_scale, c.dks, c.dvs = k_scale.data_ptr(), v_scale.data_ptr(), C.pointer(descs[2]), C.pointer(descs[3])
+    return C.byref(c)
+
+
+def _integers(t, dtype, name, count=None):
+    """A dense one-dimensional GPU tensor of integers, as an address."""
+    _require_cuda(t)
+    if t.dtype != dtype or t.dim() != 1 or not t.is_contiguous():
+        raise ValueError(f"{name} must be a dense one-dimensional tensor of {dtype}")
+    if count is not None and t.numel() != count:
+        raise ValueError(f"{name} must hold {count} numbers")
+    return t.data_ptr()
+
+
+def _tokens(k, v):
+    _require_cuda(k, v)
+    if k.dtype != v.dtype:
+        raise ValueError("K and V must have one type")
+    return _code(k)
+
+
+def cache_write(k, v, slots, k_cache, v_cache, k_scale=None, v_scale=None, stream=None):
+    """Puts tokens' K and V [tokens, heads, head_size] into the slots (int64, one per token; negative: none) of a paged cache [pages, page_size,
+    heads, head_size] of their own type, or of float8_e4m3fn or int8 with scales (float32 [pages, page_size, heads]).  See nt_cache_write."""
+    if _recorder is None:
+        st = (_calls or _load_calls()).cache_write(k, v, slots, k_cache, v_cache, k_scale, v_scale, stream)
+        if st is not None:
+            if st:
+                _check(st)
+            return k_cache, v_cache
+    import torch
+    code = _tokens(k, v)
+    _check(load().nt_cache_write(_cache(k_cache, v_cache, k_scale, v_scale), k.data_ptr(), _ref(k), v.data_ptr(), _ref(v),
+                                 _integers(slots, torch.int64, "slots", k.shape[0]), code, _stream_ptr(stream)))
+    return k_cache, v_cache
+
+
+def cache_read(k_cache, v_cache, slots, k, v, k_scale=None, v_scale=None, stream=None):
+    """K and V [tokens, heads, head_size] of the slots of a paged cache, codes times scales rounded once.  See nt_cache_read."""
+    if _recorder is None:
+        st = (_calls or _load_calls()).cache_read(k_cache, v_cache, slots, k, v, k_scale, v_scale, stream)
+        if st is not None:
+            if st:
+                _check(st)
+            return k, v
+    import torch
+    code = _tokens(k, v)
+    _check(load().nt_cache_read(_cache(k_cache, v_cache, k_scale, v_scale), k.data_ptr(), _ref(k), v.data_ptr(), _ref(v),
+                                _integers(slots, torch.int64, "slots", k.shape[0]), code, _stream_ptr(stream)))
+    return k, v
+
+
+def sdpa_paged(q, k_cache, v_cache, table, starts, lengths, out, k_scale=None, v_scale=None, scale=0.0, causal=True, window=0, max_queries=0,
+               max_length=0, stream=None):
+    """Attention of new tokens over a paged cache that holds them and their past.  q, out [tokens, query heads, head_size]; table int32 [sequences,
+    entries], starts int32 [sequences + 1] (sequence b's new tokens are starts[b] .. starts[b + 1] - 1), lengths int32 [sequences] (with the
+    new tokens).  A token sees the positions up to its own (causal), the last `window` of them (0: all).  max_queries, max_length: what
+    the host knows of the largest counts (0: nothing); they choose the kernel, not the result.  See nt_sdpa_paged."""
+    if _recorder is None:
+        st = (_calls or _load_calls()).sdpa_paged(q, k_cache, v_cache, table, starts, lengths, out, k_scale, v_scale, scale, causal, window, max_queries,
+                                                  max_length, stream)
+        if st is not None:
+            if st:
+                _check(st)
+            return out
+    import torch
+    _require_cuda(q, out, table)
+    if q.dtype != out.dtype:
+        raise ValueError("output must have the queries' dtype")
+    if table.dtype != torch.int32 or table.dim() != 2:
+        raise ValueError("table must be a two-dimensional tensor of torch.int32")
+    code = _code(q)
+    _check(load().nt_sdpa_paged(q.data_ptr(), _ref(q), _cache(k_cache, v_cache, k_scale, v_scale), table.data_ptr(), _ref(table),
+                                _integers(starts, torch.int32, "starts", table.shape[0] + 1), _integers(lengths, torch.int32, "lengths", table.shape[0]),
+                                out.data_ptr(), _ref(out), float(scale), int(bool(causal)), int(window), int(max_queries), int(max_length), code,
+                                _stream_ptr(stream)))
     return out
 
 

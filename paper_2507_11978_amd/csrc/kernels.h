@@ -97,6 +97,15 @@ nt_status launch_sdpa_desc(const void *q, const nt_tensor_desc *dq, const void *
                            const void *v, const nt_tensor_desc *dv, void *o, const nt_tensor_desc *dout,
                            float scale, int dtype, void *stream);
 
+// paged key / value cache: writing / reading it, and attention over it
+nt_status launch_cache(bool write, const nt_paged_cache *c, const void *k, const nt_tensor_desc *dk, const void *v, const nt_tensor_desc *dv,
+                       const int64_t *slots, int dtype, void *stream);
+nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_paged_cache *c, const int32_t *table, const nt_tensor_desc *dt,
+                            const int32_t *starts, const int32_t *lengths, void *out, const nt_tensor_desc *dout,
+                            float scale, int causal, int64_t window, int64_t max_queries, int64_t max_length, int dtype, void *stream);
+nt_status check_cache(const nt_paged_cache *c, int dtype, int *kind);     // kind: a CacheKind
+const nt_paged_plan &last_paged_plan();
+
 // workgroup index -> logical program id (shared by host query and device code)
 // Position seq of the tile sequence -> program id: the grid is walked in bands of up to 8 tile
 // rows, column by column inside a band, so that programs that run at the same time share operand

@@ -625,6 +625,32 @@ nt_status nt_sdpa(const void *q, const nt_tensor_desc *dq, const void *k, const 
     return nt::launch_sdpa_desc(q, dq, k, dk, v, dv, o, dout, scale, dtype, hip_stream);
 }
 
+nt_status nt_cache_write(const nt_paged_cache *cache, const void *k, const nt_tensor_desc *dk, const void *v, const nt_tensor_desc *dv,
+                         const int64_t *slots, nt_dtype dtype, void *hip_stream)
+{
+    return nt::launch_cache(true, cache, k, dk, v, dv, slots, dtype, hip_stream);
+}
+
+nt_status nt_cache_read(const nt_paged_cache *cache, void *k, const nt_tensor_desc *dk, void *v, const nt_tensor_desc *dv,
+                        const int64_t *slots, nt_dtype dtype, void *hip_stream)
+{
+    return nt::launch_cache(false, cache, k, dk, v, dv, slots, dtype, hip_stream);
+}
+
+nt_status nt_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_paged_cache *cache, const int32_t *table, const nt_tensor_desc *d_table,
+                        const int32_t *starts, const int32_t *lengths, void *out, const nt_tensor_desc *dout,
+                        float scale, int32_t causal, int64_t window, int64_t max_queries, int64_t max_length, nt_dtype dtype, void *hip_stream)
+{
+    return nt::launch_sdpa_paged(q, dq, cache, table, d_table, starts, lengths, out, dout, scale, causal, window, max_queries, max_length, dtype, hip_stream);
+}
+
+nt_status nt_last_paged_plan(nt_paged_plan *out)
+{
+    if (!out) return fail(NT_ERR_INVALID_ARG, "null output pointer");
+    *out = nt::last_paged_plan();
+    return NT_OK;
+}
+
 nt_status nt_bmm(const void *A, const nt_tensor_desc *dA, const void *B, const nt_tensor_desc *dB,
                  void *C, const nt_tensor_desc *dC, nt_dtype in_dtype, nt_dtype out_dtype,
                  nt_tile_cfg cfg, void *hip_stream)

@@ -1,0 +1,384 @@
+// Attention over a paged cache for many query rows: chunks of new tokens, whole prompts.
+//
+// A tile is 128 rows (token, query head of the group) of one sequence and key head, 32 to a wavefront, so that what the group shares is loaded once; the
+// program walks the keys that some row sees in blocks of 64 (32 at head size 256).  Arithmetic and layout are those of attention.hip: everything
+// transposed, S^T = K Q^T with the query on the lane axis, weights against a reference M that lags behind the running maximum (raised when a
+// block holds a score 15 above it), packed weights as they are for O^T += V^T P^T.  Blocks that every row of a wavefront sees are not masked; those that none
+// sees are not computed.  With an 8-bit cache the codes are widened on their way to LDS, a key's scale multiplies its scores in fp32 and a value's scale
+// its weight, so that nothing is rounded but the weights, as in a 16-bit cache.
+//
+// K and V travel through registers, one block ahead of the arithmetic, into one of two LDS copies each.  What bounds it is the matrix pipe: per block and
+// wavefront 32 instructions of 32 cycles (128 elements) beside some 90 vector instructions.
+#pragma once
+#include "paged.h"
+
+namespace nt {
+
+constexpr int kManyWaves = 4, kManyRows = 32 * kManyWaves;
+constexpr int many_keys(int size) { return size == 256 ? 32 : 64; }
+constexpr size_t many_block(int size) { return (size_t)many_keys(size) * size * 2; }
+// [K0][K1][V0][V1], scales of two blocks (K's, then V's), three flags
+constexpr size_t many_lds(int size) { return 4 * many_block(size) + 2 * 2 * many_keys(size) * 4 + 16; }
+
+template <bool BF16, int KIND, int SIZE>
+__global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 : 1) void paged_many_kernel(const PagedArgs g)
+{
+    constexpr int KB = many_keys(SIZE), JB = KB / 32, CH = SIZE / 8, PER = KB * CH / 256, RSTEP = 256 / CH;
+    constexpr int ES = KIND == CACHE_SAME ? 2 : 1;
+    constexpr uint32_t BLK = many_block(SIZE);
+    constexpr bool NORM = KIND != CACHE_SAME && !BF16;
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    float *const scales = reinterpret_cast<float *>(smem + 4 * BLK);
+    int *const flags = reinterpret_cast<int *>(scales + 4 * KB);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hi = lane >> 5;
+
+    // ---- which tile: head fastest (a head's tiles on one XCD, where the heads are a multiple of 8), then share, then tile, the sequences' last first: they
+    // see the most keys.
+    int w = blockIdx.x;
+    const int h = w % g.Hkv;
+    w /= g.Hkv;
+    const int split = w % g.splits, number = g.tiles - 1 - w / g.splits;
+    auto tiles_before = [&](int b) { return first_tile(g.starts, b, g.T, g.G, kManyRows); };
+    int b = 0;
+    for (int up = g.B; up - b > 1;) {                                      // 64 sequences at a time: the last whose tiles begin at or before this one
+        const int step = (up - b + 63) / 64, at = b + lane * step;
+        const uint64_t below = __ballot(at < up && tiles_before(at < up ? at : b) <= number);
+        const int found = below ? 63 - __builtin_clzll(below) : 0;
+        b += found * step;
+        up = b + step < up ? b + step : up;
+    }
+    const Sequence seq = sequence_of(g, b);
+    const int64_t r0_64 = (int64_t)(number - tiles_before(b)) * kManyRows;
+    const int rows_all = seq.count * g.G;
+    if (r0_64 < 0 || r0_64 >= rows_all) return;                            // (workgroup-uniform)
+    const int r0 = (int)r0_64, tile_last = r0 + kManyRows < rows_all ? r0 + kManyRows - 1 : rows_all - 1;
+    const int32_t *pages = g.table + (int64_t)b * g.t_sb;
+    const char *Kh = g.K + (int64_t)h * g.k_sh * ES, *Vh = g.V + (int64_t)h * g.v_sh * ES;
+    const int32_t tile_i0 = (int32_t)divide(r0, g.group), tile_i1 = (int32_t)divide(tile_last, g.group);
+    const KeyRange keys = keys_of(g, seq, tile_i0, tile_i1, split, KB);
+    // keys that every row of the tile sees: [seen_lo, seen_hi)
+    const int32_t seen_lo = keys_seen(seq, tile_i1, g.causal, g.window).lo, seen_hi = keys_seen(seq, tile_i0, g.causal, g.window).hi;
+
+    // ---- this lane's row and its keys [row_lo, row_hi); the wavefront's: seen by some row [wave_lo, wave_hi), by all [all_lo, all_hi)
+    const int row = r0 + 32 * wave + l32;
+    const bool real = row < rows_all;
+    const bool busy = r0 + 32 * wave < rows_all;                           // wavefront-uniform
+    const uint32_t rc = real ? row : tile_last, mine = divide(rc, g.group), head = h * g.G + (rc - mine * g.group.d);
+    const KeyRange row_keys = keys_seen(seq, (int32_t)mine, g.causal, g.window);
+    const int32_t row_lo = row_keys.lo, row_hi = row_keys.hi;
+    const int32_t all_lo = __builtin_amdgcn_readlane(row_lo, 31), all_hi = __builtin_amdgcn_readlane(row_hi, 0);
+    const int32_t wave_lo = __builtin_amdgcn_readlane(row_lo, 0), wave_hi = __builtin_amdgcn_readlane(row_hi, 31);
+    const int64_t token = seq.first + (int32_t)mine;
+
+    u32x4 qf[SIZE / 16];
+    {
+        const uint16_t *q = g.Q + token * g.q_st + (int64_t)head * g.q_sh;
+#pragma unroll
+        for (int ks = 0; ks < SIZE / 16; ++ks) {
+            qf[ks] = u32x4{0, 0, 0, 0};
+            if (16 * ks + 8 * hi < g.D) __builtin_memcpy(&qf[ks], q + 16 * ks + 8 * hi, 16);
+        }
+    }
+
+    // ---- a block on its way: thread tid moves chunk tid % CH of rows tid / CH + u * RSTEP
+    const int ch = tid % CH, row0 = tid / CH;
+    typedef typename std::conditional<KIND == CACHE_SAME, u32x4, u32x2>::type Piece;
+    Piece kr[PER], vr[PER];
+    float sc = 0.f;
+    int32_t id[PER], sid = -1;                                             // pages of the block that is fetched next; sid: of the thread's scale
+    bool named[PER], inside[PER];
+    auto find = [&](int kb) {
+#pragma unroll
+        for (int u = 0; u < PER; ++u) id[u] = page_at(pages, divide((uint32_t)(kb * KB + row0 + u * RSTEP), g.page), g.width, g.pages);
+        if constexpr (KIND != CACHE_SAME) sid = page_at(pages, divide((uint32_t)(kb * KB + tid % KB), g.page), g.width, g.pages);
+    };
+    auto fetch = [&](int kb) {
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            const int32_t key = kb * KB + row0 + u * RSTEP;
+            named[u] = id[u] >= 0;
+            inside[u] = key >= keys.lo && key < keys.hi;
+            const int64_t page = named[u] ? id[u] : 0, at = (uint32_t)key - divide((uint32_t)key, g.page) * g.page.d;
+            kr[u] = vr[u] = Piece{};
+            if (8 * ch < g.D) {
+                __builtin_memcpy(&kr[u], Kh + (page * g.k_sp + at * g.k_ss + 8 * ch) * ES, sizeof(Piece));
+                __builtin_memcpy(&vr[u], Vh + (page * g.v_sp + at * g.v_ss + 8 * ch) * ES, sizeof(Piece));
+            }
+        }
+        if constexpr (KIND != CACHE_SAME) {
+            if (tid < 2 * KB) {
+                const uint32_t key = kb * KB + tid % KB;
+                const int64_t page = sid >= 0 ? sid : 0, at = key - divide(key, g.page) * g.page.d;
+                sc = tid < KB ? g.KS[page * g.ks_sp + at * g.ks_ss + (int64_t)h * g.ks_sh] : g.VS[page * g.vs_sp + at * g.vs_ss + (int64_t)h * g.vs_sh];
+            }
+        }
+    };
+    // into LDS copy `copy`.  Keys that no page is named for become NaN, their values, and those of keys outside the range, zeros (see paged_few.h)
+    auto stash = [&](int kb, uint32_t copy) {
+        const bool hidden = kb * KB < seen_lo || kb * KB + KB > seen_hi;   // from some row
+        bool odd = false;
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            u32x4 k, v;
+            if constexpr (KIND == CACHE_SAME) {
+                k = kr[u];
+                v = vr[u];
+            } else {
+                k = widen8<BF16, KIND>(kr[u]);
+                v = widen8<BF16, KIND>(vr[u]);
+            }
+            k = named[u] ? k : u32x4{kNanPair, kNanPair, kNanPair, kNanPair};
+            v = named[u] && inside[u] ? v : u32x4{0, 0, 0, 0};
+            if (hidden) odd = odd || any_not_finite<BF16>(v);
+            const uint32_t at = lds_at<SIZE>(row0 + u * RSTEP, ch);
+            lds_write16(smem, copy * BLK + at, k);
+            lds_write16(smem, (2 + copy) * BLK + at, v);
+        }
+        if constexpr (KIND != CACHE_SAME)
+            if (tid < 2 * KB) scales[copy * 2 * KB + tid] = sc;
+        if (odd) flags[kb % 3] = 1;
+    };
+
+    float16v ot[SIZE / 32];
+#pragma unroll
+    for (int db = 0; db < SIZE / 32; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) ot[db][v] = 0.f;
+    float m_ref = -INFINITY, l_run = 0.f;                                  // reference (-inf: none yet) and sum (8-bit caches: of this lane's keys)
+    float unit = 0.f, per_unit = 0.f;                                      // of this lane's row, see paged_few.h
+    bool pending = true;                                                   // wavefront-uniform: some row has no reference
+    const uint32_t one_pair = ((lane >> 4) & 1) == ((lane >> 2) & 1) ? (BF16 ? 0x3f803f80u : 0x3c003c00u) : 0u;
+    const u32x4 ones{one_pair, one_pair, one_pair, one_pair};              // (the sum of query lane % 32 in every lane: see attention.hip)
+    const int gq = lane >> 4, li = lane & 15;
+    const uint32_t v_key = 4 * (gq >> 1) + (li >> 2), v_chunk = 2 * (gq & 1) + ((li >> 1) & 1), v_half = (li & 1) * 8;
+
+    auto compute = [&](const int kb, const uint32_t copy) __attribute__((always_inline)) {
+        const int base = kb * KB;
+        const char *ks_lds = smem + copy * BLK, *vs_lds = smem + (2 + copy) * BLK;
+        // ---- S^T: st[jb][v] <-> key 32 jb + 8 (v / 4) + 4 hi + v % 4, query l32
+        float16v st[JB];
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb) {
+#pragma unroll
+            for (int v = 0; v < 16; ++v) st[jb][v] = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < SIZE / 16; ++ks) st[jb] = mfma32<BF16>(lds_read16(ks_lds, lds_at<SIZE>(32 * jb + l32, 2 * ks + hi)), qf[ks], st[jb]);
+        }
+        if constexpr (KIND != CACHE_SAME) {
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const float4v k4 = *reinterpret_cast<const float4v *>(&scales[copy * 2 * KB + 32 * jb + 8 * q + 4 * hi]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) st[jb][4 * q + e] *= k4[e];
+                }
+        }
+        const bool hidden = base < all_lo || base + KB > all_hi;          // wavefront-uniform: from some row
+        if (hidden) {
+            const float out = g.scale_log2e >= 0.f ? -INFINITY : INFINITY;
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int32_t key = base + 32 * jb + 8 * (v / 4) + 4 * hi + (v % 4);
+                    if (key < row_lo || key >= row_hi) st[jb][v] = out;
+                }
+        }
+        const bool careful = hidden && flags[kb % 3] != 0;
+        if constexpr (NORM) {
+            const float *vs = &scales[copy * 2 * KB + KB];
+            float top = 0.f;                                               // the largest scale that the row sees
+            if (hidden) {
+#pragma unroll
+                for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int j = 32 * jb + 8 * (v / 4) + 4 * hi + (v % 4);
+                        if (base + j >= row_lo && base + j < row_hi) top = fmaxf(top, __builtin_fabsf(vs[j]));
+                    }
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+            } else {
+                if (lane < KB) top = __builtin_fabsf(vs[lane]);
+#pragma unroll
+                for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+            }
+            if (__any(top > unit)) {
+                const float grown = top > unit ? unit_above(top) : unit, shrink = unit == 0.f ? 0.f : unit / grown;
+                unit = grown;
+                per_unit = grown == 0.f ? 0.f : 1.f / grown;
+#pragma unroll
+                for (int db = 0; db < SIZE / 32; ++db)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) ot[db][v] *= shrink;
+            }
+        }
+        // ---- weights, packed (8-bit caches: times the values' scales), and their sum
+        u32x4 pk[JB][2];
+        float rs;
+        auto exponentials = [&](const float m) {
+            float sum = 0.f;
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        float p[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[jb][8 * s2 + 4 * q + e], g.scale_log2e, -m));
+                        if constexpr (KIND != CACHE_SAME) {
+                            sum += (p[0] + p[1]) + (p[2] + p[3]);
+                            const float4v v4 = *reinterpret_cast<const float4v *>(&scales[copy * 2 * KB + KB + 32 * jb + 16 * s2 + 8 * q + 4 * hi]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float x = p[e] * (NORM ? v4[e] * per_unit : v4[e]);
+                                // (the scale of a hidden key may be anything; that of a seen one with a weight of 0 hides no NaN either way)
+                                p[e] = hidden && p[e] == 0.f ? 0.f : x;
+                            }
+                        }
+                        pk[jb][s2][2 * q] = pack_two<BF16>(p[0], p[1]);
+                        pk[jb][s2][2 * q + 1] = pack_two<BF16>(p[2], p[3]);
+                    }
+            if constexpr (KIND != CACHE_SAME) rs = sum;
+        };
+        // the sums of the packed weights on the matrix pipe; `apart`: queries 0 .. 15 and 16 .. 31 by instructions of their own (0 * NaN is NaN: what
+        // one holds would reach the other; the sums are the same bits either way)
+        auto matrix_sum = [&](bool apart) {
+            float4v sum[2]{};
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                if (half && !apart) break;
+#pragma unroll
+                for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                    for (int s2 = 0; s2 < 2; ++s2)
+                        sum[half] = mfma16<BF16>(ones, !apart || (l32 >> 4) == half ? pk[jb][s2] : u32x4{0, 0, 0, 0}, sum[half]);
+            }
+            return apart && l32 >= 16 ? sum[1][0] : sum[0][0];
+        };
+        // A row's weights, sum and reference depend on that row alone, also where a neighbour in the wavefront needs its reference raised.
+        bool accept = false;
+        if (!pending) {
+            exponentials(m_ref);
+            if constexpr (KIND == CACHE_SAME) rs = matrix_sum(false);
+            accept = __all(rs < 32768.f);
+        }
+        if (!accept) {                                                     // wavefront-uniform: a row without reference, or a score far above M
+            bool keep = false;                                             // this row's reference is close enough
+            if (__any(m_ref != -INFINITY)) {
+                exponentials(m_ref == -INFINITY ? 0.f : m_ref);
+                if constexpr (KIND == CACHE_SAME) rs = matrix_sum(true);
+                keep = m_ref != -INFINITY && rs < 32768.f;
+                if constexpr (KIND != CACHE_SAME) keep = keep && __shfl_xor(rs, 32, 64) < 32768.f;
+            }
+            float mx = -INFINITY;
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) mx = fmaxf(mx, st[jb][v] * g.scale_log2e);
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            const float m_new = keep ? m_ref : fmaxf(m_ref, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+            const float alpha = __builtin_amdgcn_exp2f(m_ref - m_use);
+            exponentials(m_use);
+            if constexpr (KIND == CACHE_SAME) rs = matrix_sum(true);
+            l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < SIZE / 32; ++db)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) ot[db][v] *= alpha;
+            m_ref = m_new;
+            pending = __any(m_new == -INFINITY);
+        }
+        l_run += rs;
+        // ---- O^T += V^T P^T: k step (jb, s2) lists its 16 keys as 32 jb + 16 s2 + 8 part + 4 hi + 0 .. 3
+#pragma unroll
+        for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+            for (int s2 = 0; s2 < 2; ++s2)
+#pragma unroll
+                for (int db = 0; db < SIZE / 32; ++db) {
+                    u32x2 a = lds_read_transposed(vs_lds, lds_at<SIZE>(32 * jb + 16 * s2 + v_key, 4 * db + v_chunk) + v_half);
+                    u32x2 c = lds_read_transposed(vs_lds, lds_at<SIZE>(32 * jb + 16 * s2 + 8 + v_key, 4 * db + v_chunk) + v_half);
+                    if (careful) {
+                        a = u32x2{without_not_finite<BF16>(a[0]), without_not_finite<BF16>(a[1])};
+                        c = u32x2{without_not_finite<BF16>(c[0]), without_not_finite<BF16>(c[1])};
+                    }
+                    ot[db] = mfma32<BF16>(u32x4{a[0], a[1], c[0], c[1]}, pk[jb][s2], ot[db]);
+                }
+        if (careful) {
+            // infinities and NaN of keys that only some rows see: added to those rows alone
+#pragma unroll 1
+            for (int key = 0; key < KB; ++key) {
+                const bool sees = base + key >= row_lo && base + key < row_hi;
+#pragma unroll
+                for (int db = 0; db < SIZE / 32; ++db)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        u32x2 v;
+                        __builtin_memcpy(&v, vs_lds + lds_at<SIZE>(key, 4 * db + q) + hi * 8, 8);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float x = only_not_finite(widen_one<BF16>(v[e >> 1], e & 1));
+                            ot[db][4 * q + e] += sees ? x : 0.f;
+                        }
+                    }
+            }
+        }
+    };
+
+    const int k_end = keys.lo < keys.hi ? (keys.hi + KB - 1) / KB : 0;
+    int kb = keys.lo < keys.hi ? keys.lo / KB : 0;
+    if (tid < 3) flags[tid] = 0;
+    __syncthreads();
+    if (kb < k_end) {                                                      // (workgroup-uniform, as the loop's count)
+        find(kb);
+        fetch(kb);
+        find(kb + 1);
+        stash(kb, 0);
+    }
+    __syncthreads();
+    for (uint32_t copy = 0; kb < k_end; ++kb, copy ^= 1) {
+        const bool more = kb + 1 < k_end;
+        if (more) {
+            fetch(kb + 1);
+            find(kb + 2);
+        }
+        if (busy && kb * KB < wave_hi && kb * KB + KB > wave_lo) compute(kb, copy);
+        if (tid == 0) flags[(kb + 2) % 3] = 0;                             // (read in the pass before this one, set in the next)
+        if (more) stash(kb + 1, copy ^ 1);
+        __syncthreads();
+    }
+
+    // ---- O = O^T / l, stored along d: after the half-wavefronts trade register groups a lane owns d = 32 db + 16 hi .. + 15 of its row
+    const float total = KIND == CACHE_SAME ? l_run : l_run + __shfl_xor(l_run, 32, 64);
+    const float factor = (g.splits > 1 ? 1.f : total == 0.f ? 0.f : 1.0f / total) * (NORM ? unit : 1.f);
+    const int64_t at = (token * g.Hq + head) * g.splits + split;
+    if (g.splits > 1 && real && hi == 0) *reinterpret_cast<float2v *>(g.part_ml + 2 * at) = float2v{m_ref, total};
+#pragma unroll
+    for (int db = 0; db < SIZE / 32; ++db) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) ot[db][v] *= factor;
+        uint32_t o[16];
+        gather_row16(ot[db], o);                                           // (all lanes take part)
+        const int d = 32 * db + 16 * hi;
+        if (!real || d >= g.D) continue;
+        if (g.splits > 1) {
+            float *dst = g.part_o + at * g.D + d;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (d + 4 * i < g.D) __builtin_memcpy(dst + 4 * i, &o[4 * i], 16);
+        } else {
+            uint16_t *dst = g.O + token * g.o_st + (int64_t)head * g.o_sh + d;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                u32x4 x;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] = pack_two<BF16>(__builtin_bit_cast(float, o[8 * i + 2 * j]), __builtin_bit_cast(float, o[8 * i + 2 * j + 1]));
+                if (d + 8 * i < g.D) __builtin_memcpy(dst + 8 * i, &x, 16);
+            }
+        }
+    }
+}
+
+}  // namespace nt

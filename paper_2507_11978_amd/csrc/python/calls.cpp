@@ -26,6 +26,9 @@ decltype(&nt_softmax) p_softmax;
 decltype(&nt_rms_norm) p_rms_norm;
 decltype(&nt_add) p_add;
 decltype(&nt_silu) p_silu;
+decltype(&nt_cache_write) p_cache_write;
+decltype(&nt_cache_read) p_cache_read;
+decltype(&nt_sdpa_paged) p_sdpa_paged;
 
 struct Operand {
     void *p;
@@ -33,20 +36,21 @@ struct Operand {
     nt_dtype dtype;
 };
 
-// false: not a plain GPU tensor of a type the library knows
-bool take(PyObject *o, Operand *out)
+// false: not a plain GPU tensor
+bool plain(PyObject *o, const at::Tensor **out)
 {
     if (!THPVariable_CheckExact(o)) return false;
     const at::Tensor &t = THPVariable_Unpack(o);
     if (!t.defined() || !t.is_cuda() || !t.has_storage()) return false;
     const c10::TensorImpl *impl = t.unsafeGetTensorImpl();
     if (impl->has_symbolic_sizes_strides() || impl->key_set().has(c10::DispatchKey::Python)) return false;
-    switch (t.scalar_type()) {
-    case at::kHalf: out->dtype = NT_F16; break;
-    case at::kBFloat16: out->dtype = NT_BF16; break;
-    case at::kFloat: out->dtype = NT_F32; break;
-    default: return false;
-    }
+    *out = &t;
+    return true;
+}
+
+// false: no tensor that a descriptor can tell of
+bool describe(const at::Tensor &t, Operand *out)
+{
     const int64_t n = t.dim();
     if (n < 1 || n > NT_MAX_DIMS) return false;
     const auto sizes = t.sizes(), strides = t.strides();
@@ -59,6 +63,66 @@ bool take(PyObject *o, Operand *out)
     return true;
 }
 
+// false: not a plain GPU tensor of a type the library knows
+bool take(PyObject *o, Operand *out)
+{
+    const at::Tensor *t;
+    if (!plain(o, &t)) return false;
+    switch (t->scalar_type()) {
+    case at::kHalf: out->dtype = NT_F16; break;
+    case at::kBFloat16: out->dtype = NT_BF16; break;
+    case at::kFloat: out->dtype = NT_F32; break;
+    default: return false;
+    }
+    return describe(*t, out);
+}
+
+// one tensor of a paged cache
+bool take_cache(PyObject *o, Operand *out)
+{
+    const at::Tensor *t;
+    if (!plain(o, &t)) return false;
+    switch (t->scalar_type()) {
+    case at::kHalf: out->dtype = NT_F16; break;
+    case at::kBFloat16: out->dtype = NT_BF16; break;
+    case at::kFloat8_e4m3fn: out->dtype = NT_E4M3; break;
+    case at::kChar: out->dtype = NT_I8; break;
+    default: return false;
+    }
+    return describe(*t, out);
+}
+
+// a tensor of integers of the given type and rank
+bool take_integers(PyObject *o, at::ScalarType type, int64_t ndim, Operand *out)
+{
+    const at::Tensor *t;
+    return plain(o, &t) && t->scalar_type() == type && t->dim() == ndim && describe(*t, out);
+}
+
+// ... dense, of `count` numbers
+bool take_list(PyObject *o, at::ScalarType type, int64_t count, Operand *out)
+{
+    return take_integers(o, type, 1, out) && out->d.size[0] == count && (count < 2 || out->d.stride[0] == 1);
+}
+
+struct Paged {
+    Operand k, v, ks, vs;
+    nt_paged_cache c;
+};
+
+bool take_paged(PyObject *k, PyObject *v, PyObject *ks, PyObject *vs, Paged *out)
+{
+    if (!take_cache(k, &out->k) || !take_cache(v, &out->v) || out->k.dtype != out->v.dtype) return false;
+    out->c = nt_paged_cache{out->k.p, out->v.p, &out->k.d, &out->v.d, nullptr, nullptr, nullptr, nullptr, out->k.dtype};
+    if (ks == Py_None && vs == Py_None) return true;
+    if (!take(ks, &out->ks) || !take(vs, &out->vs) || out->ks.dtype != NT_F32 || out->vs.dtype != NT_F32) return false;
+    out->c.k_scale = (float *)out->ks.p;
+    out->c.v_scale = (float *)out->vs.p;
+    out->c.dks = &out->ks.d;
+    out->c.dvs = &out->vs.d;
+    return true;
+}
+
 bool integer(PyObject *o, int32_t *v)
 {
     if (!PyLong_CheckExact(o)) return false;
@@ -67,6 +131,14 @@ bool integer(PyObject *o, int32_t *v)
     if (overflow || x < INT32_MIN || x > INT32_MAX) return false;
     *v = (int32_t)x;
     return true;
+}
+
+bool long_integer(PyObject *o, int64_t *v)
+{
+    if (!PyLong_CheckExact(o)) return false;
+    int overflow = 0;
+    *v = PyLong_AsLongAndOverflow(o, &overflow);
+    return !overflow;
 }
 
 bool real(PyObject *o, float *v)
@@ -225,15 +297,65 @@ PyObject *silu(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// bind(addresses of nt_gemm, nt_bmm, nt_addmm, nt_addmm_act, nt_conv2d_implicit, nt_sdpa, nt_softmax, nt_rms_norm, nt_add, nt_silu)
+// cache_write(k, v, slots, k_cache, v_cache, k_scale, v_scale, stream)
+PyObject *cache_write(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        Operand k, v, slots;
+        Paged c;
+        void *s;
+        if (!p_cache_write || n != 8 || !take(a[0], &k) || !take(a[1], &v) || k.dtype != v.dtype || !take_list(a[2], at::kLong, k.d.size[0], &slots) ||
+            !take_paged(a[3], a[4], a[5], a[6], &c) || !stream_of(a[7], &s))
+            return declined();
+        return without_lock([&] { return p_cache_write(&c.c, k.p, &k.d, v.p, &v.d, (const int64_t *)slots.p, k.dtype, s); });
+    });
+}
+
+// cache_read(k_cache, v_cache, slots, k, v, k_scale, v_scale, stream)
+PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        Operand k, v, slots;
+        Paged c;
+        void *s;
+        if (!p_cache_read || n != 8 || !take(a[3], &k) || !take(a[4], &v) || k.dtype != v.dtype || !take_list(a[2], at::kLong, k.d.size[0], &slots) ||
+            !take_paged(a[0], a[1], a[5], a[6], &c) || !stream_of(a[7], &s))
+            return declined();
+        return without_lock([&] { return p_cache_read(&c.c, k.p, &k.d, v.p, &v.d, (const int64_t *)slots.p, k.dtype, s); });
+    });
+}
+
+// sdpa_paged(q, k_cache, v_cache, table, starts, lengths, out, k_scale, v_scale, scale, causal, window, max_queries, max_length, stream)
+PyObject *sdpa_paged(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        Operand q, table, starts, lengths, o;
+        Paged c;
+        float scale;
+        int64_t window, queries, length;
+        void *s;
+        if (!p_sdpa_paged || n != 15 || !take(a[0], &q) || !take_paged(a[1], a[2], a[7], a[8], &c) || !take_integers(a[3], at::kInt, 2, &table) ||
+            !take_list(a[4], at::kInt, table.d.size[0] + 1, &starts) || !take_list(a[5], at::kInt, table.d.size[0], &lengths) || !take(a[6], &o) ||
+            o.dtype != q.dtype || !real(a[9], &scale) || !PyBool_Check(a[10]) || !long_integer(a[11], &window) || !long_integer(a[12], &queries) ||
+            !long_integer(a[13], &length) || !stream_of(a[14], &s))
+            return declined();
+        return without_lock([&] {
+            return p_sdpa_paged(q.p, &q.d, &c.c, (const int32_t *)table.p, &table.d, (const int32_t *)starts.p, (const int32_t *)lengths.p, o.p, &o.d, scale,
+                                a[10] == Py_True, window, queries, length, q.dtype, s);
+        });
+    });
+}
+
+// bind(addresses of nt_gemm, nt_bmm, nt_addmm, nt_addmm_act, nt_conv2d_implicit, nt_sdpa, nt_softmax, nt_rms_norm, nt_add, nt_silu,
+// nt_cache_write, nt_cache_read, nt_sdpa_paged)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    if (n != 10) {
-        PyErr_SetString(PyExc_TypeError, "ten addresses wanted");
+    if (n != 13) {
+        PyErr_SetString(PyExc_TypeError, "thirteen addresses wanted");
         return nullptr;
     }
-    void *p[10];
-    for (int i = 0; i < 10; ++i) {
+    void *p[13];
+    for (int i = 0; i < 13; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (!p[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address");
@@ -243,12 +365,13 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
     p_gemm = (decltype(p_gemm))p[0]; p_bmm = (decltype(p_bmm))p[1]; p_addmm = (decltype(p_addmm))p[2]; p_addmm_act = (decltype(p_addmm_act))p[3];
     p_conv = (decltype(p_conv))p[4]; p_sdpa = (decltype(p_sdpa))p[5]; p_softmax = (decltype(p_softmax))p[6]; p_rms_norm = (decltype(p_rms_norm))p[7];
     p_add = (decltype(p_add))p[8]; p_silu = (decltype(p_silu))p[9];
+    p_cache_write = (decltype(p_cache_write))p[10]; p_cache_read = (decltype(p_cache_read))p[11]; p_sdpa_paged = (decltype(p_sdpa_paged))p[12];
     Py_RETURN_NONE;
 }
 
 #define NT_CALL(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {NT_CALL(gemm), NT_CALL(bmm), NT_CALL(addmm), NT_CALL(conv2d), NT_CALL(sdpa), NT_CALL(softmax), NT_CALL(rms_norm),
-                         NT_CALL(add), NT_CALL(silu), NT_CALL(bind), {nullptr, nullptr, 0, nullptr}};
+                         NT_CALL(add), NT_CALL(silu), NT_CALL(cache_write), NT_CALL(cache_read), NT_CALL(sdpa_paged), NT_CALL(bind), {nullptr, nullptr, 0, nullptr}};
 #undef NT_CALL
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_nt_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
