@@ -99,6 +99,8 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     a.width = (int32_t)W; a.pages = (int32_t)pages;
     a.causal = causal ? 1 : 0;
     a.window = (int32_t)std::min<int64_t>(window, 1 << 30);
+    const int64_t es = kind == CACHE_SAME ? 2 : 1, most_bytes = (1LL << 31) - 4096;
+    a.uniform = page_size % 16 == 0 && a.k_ss >= 0 && a.k_ss < most_bytes / (16 * es) && a.v_ss >= 0 && a.v_ss < most_bytes / (16 * es);
     a.page = divider_of((uint32_t)page_size);
     a.group = divider_of((uint32_t)a.G);
     a.scale_log2e = (scale == 0.f ? 1.0f / sqrtf((float)D) : scale) * 1.4426950408889634f;
@@ -110,10 +112,11 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     const int64_t base = (int64_t)a.tiles * Hkv;
     if (base > kMaxWorkgroups) return fail(NT_ERR_UNSUPPORTED, "too many programs for one launch");
     // ---- shares
+    const int built = D <= 64 ? 64 : D <= 128 ? 128 : 256;
     int64_t length = W * page_size;
     if (max_length) length = std::min(length, max_length);
     if (window) length = std::min(length, window + most);
-    const int64_t block = rows == kManyRows ? many_keys(D <= 64 ? 64 : D <= 128 ? 128 : 256) : kFewKeys;
+    const int64_t block = rows == kManyRows ? many_keys(built) : few_trip(kind, built);
     const int64_t wanted = rows == kManyRows ? (base >= 256 ? 1 : 512 / base) : (1024 + base - 1) / base;
     int64_t splits = std::max<int64_t>(1, std::min(wanted, length / (rows == kManyRows ? 512 : 256)));
     splits = std::min<int64_t>(splits, kMaxWorkgroups / base);

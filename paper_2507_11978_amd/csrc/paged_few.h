@@ -1,34 +1,45 @@
 // Attention over a paged cache for few query rows per key head: a decoding step, or a few tokens of each sequence.
 //
 // One program per (sequence, key head, share of the keys) has the rows (token, query head of the group) of that sequence, 16 or 32 at a time, so that
-// K and V are read once for all query heads that share them.  Its four wavefronts take tiles of 32 keys in turn, each with a running maximum m (base-2
+// K and V are read once for all query heads that share them.  Its four wavefronts take the keys in turn, tiles of 32, each with a running maximum m (base-2
 // units), sum l and accumulator of its own:
 //   S^T = K Q^T;  p = 2^(c S - m);  l += sum p;  O^T += V^T P^T,
 // brought to a common maximum at the end.  16 x 16 x 32 matrix instructions with the query on the lane axis (lane % 16): the four scores that a lane holds
 // of each 16 keys are, packed, its part of the second product's operand, if the other operand lists the keys in the same order.
 //
 // K goes from memory straight into the operand's registers (a lane holds its key's elements).  V has to be turned: through registers into LDS, a region per
-// wavefront, and out with transposing reads; no barrier in the loop.  The next tile's loads are issued as soon as this one's registers are free, before
-// its exponentials and the second product.  What bounds it is memory: per tile a wavefront has some 150 vector instructions and 16 matrix
-// instructions for 16 KB (128 elements of 16 bits), a tenth of the time that the unit's share of memory takes to bring them.
+// wavefront, and out with transposing reads; no barrier in the loop.  A trip takes as many tiles as make 16 KB of K and V, all of them in flight at once: K's
+// loads for the next trip go out once the scores are there, V's as its registers empty into LDS.
 #pragma once
 #include "paged.h"
 
 namespace nt {
 
-constexpr int kFewWaves = 4, kFewKeys = 32;
-constexpr size_t few_lds(int size, int mb) { return (size_t)kFewWaves * mb * 64 * size; }        // V's tile (64 * size bytes), later 16 * mb rows of fp32 outputs
+constexpr int kFewWaves = 4;
+constexpr size_t few_lds(int size, int mb) { return (size_t)kFewWaves * mb * 64 * size; }        // V's 32 keys (64 * size bytes), later 16 * mb rows of fp32 outputs
+// 32-key tiles of a trip, which a wavefront has in flight: two, or one where a tile of K and V is 16 KB
+constexpr int few_tiles(int kind, int size) { return size * (kind == CACHE_SAME ? 2 : 1) >= 256 ? 1 : 2; }
+constexpr int few_trip(int kind, int size) { return 32 * few_tiles(kind, size); }        // keys
 
-template <bool BF16, int KIND, int SIZE, int MB>
+// a * s, 32 by 64 bits
+__device__ __forceinline__ int64_t times(uint32_t a, int64_t s)
+{
+    return (int64_t)((uint64_t)a * (uint32_t)s + ((uint64_t)(a * (uint32_t)((uint64_t)s >> 32)) << 32));
+}
+
+// UNIFORM: page_size is a multiple of 16, so that 16 keys that begin at a multiple of 16 lie on one page: the table is read and the addresses are made
+// once for a wavefront, on the scalar unit, and a lane's part is an offset that never changes.
+template <bool BF16, int KIND, int SIZE, int MB, bool UNIFORM>
 __global__ __launch_bounds__(64 * kFewWaves, SIZE * MB <= 128 ? 2 : 1) void paged_few_kernel(const PagedArgs g)
 {
     constexpr int KS = SIZE / 32;                                          // k steps of the first product
     constexpr int NV = KIND == CACHE_SAME ? SIZE / 32 : SIZE / 64;         // 16-byte loads per lane, 16 keys and tensor
     constexpr int ES = KIND == CACHE_SAME ? 2 : 1;
+    constexpr int NT = few_tiles(KIND, SIZE), NG = 2 * NT, TRIP = 32 * NT;   // tiles of 32 and groups of 16 keys in a trip
     constexpr bool NORM = KIND != CACHE_SAME && !BF16;                     // weights times scales may leave fp16's range: see `unit`
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     __shared__ float red_m[kFewWaves][16 * MB], red_l[kFewWaves][16 * MB];
-    __shared__ __attribute__((aligned(16))) float scales[KIND == CACHE_SAME ? 1 : kFewWaves][2 * kFewKeys];
+    __shared__ __attribute__((aligned(16))) float scales[KIND == CACHE_SAME ? 1 : kFewWaves][KIND == CACHE_SAME ? 4 : 2 * TRIP];     // K's, V's
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
     char *vt = smem + wave * (64 * SIZE * MB);
 
@@ -37,13 +48,24 @@ __global__ __launch_bounds__(64 * kFewWaves, SIZE * MB <= 128 ? 2 : 1) void page
     w /= g.Hkv;
     const int split = w % g.splits, b = w / g.splits;
     const Sequence seq = sequence_of(g, b);
+    typedef const __attribute__((address_space(4))) int32_t *ScalarTable;
     const int32_t *pages = g.table + (int64_t)b * g.t_sb;
     const int rows_all = seq.count * g.G;
     const char *Kh = g.K + (int64_t)h * g.k_sh * ES, *Vh = g.V + (int64_t)h * g.v_sh * ES;
+    const float *KSh = g.KS + (int64_t)h * g.ks_sh, *VSh = g.VS + (int64_t)h * g.vs_sh;
+    const bool full = g.D == SIZE;
+    // element offsets of this lane's loads within a row: of 16 bytes; a head size below SIZE: where it has elements, else its last ones (codes: of 8 bytes)
+    int32_t doff[NV], doff2[KIND == CACHE_SAME ? 1 : NV];
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+        const int d = KIND == CACHE_SAME ? 32 * n + 8 * g4 : 64 * n + 16 * g4;
+        doff[n] = d <= g.D - 8 ? d : g.D - 8;
+        if constexpr (KIND != CACHE_SAME) doff2[n] = d + 8 <= g.D - 8 ? d + 8 : g.D - 8;
+    }
 
     for (int r0 = 0; r0 < rows_all; r0 += 16 * MB) {                       // (one pass, unless the caller's bound on new tokens was too low)
         const int last = r0 + 16 * MB < rows_all ? r0 + 16 * MB - 1 : rows_all - 1;
-        const KeyRange keys = keys_of(g, seq, (int32_t)divide(r0, g.group), (int32_t)divide(last, g.group), split, kFewKeys);
+        const KeyRange keys = keys_of(g, seq, (int32_t)divide(r0, g.group), (int32_t)divide(last, g.group), split, TRIP);
 
         // ---- this lane's rows (row c16 of each 16): their keys [row_lo, row_hi), and Q as the first product's operand
         int32_t row_lo[MB], row_hi[MB];
@@ -80,72 +102,99 @@ __global__ __launch_bounds__(64 * kFewWaves, SIZE * MB <= 128 ? 2 : 1) void page
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) unit[mb] = per_unit[mb] = 0.f;
 
-        // ---- loads: lane (c16, g4) has key c16 of either 16 and a quarter of its elements
-        u32x4 kr[2][NV], vr[2][NV];
-        float sc = 0.f;                                                    // lanes 0 .. 31: the scale of key lane's K, 32 .. 63: of key lane - 32's V
-        int32_t id[2];                                                     // page of the tile that is fetched next
-        bool named[2], inside[2];                                          // of the tile in kr, vr: the table names its page; the key is in `keys`
+        // ---- loads: lane (c16, g4) has key c16 of each 16 and a quarter of its elements
+        u32x4 kr[NG][NV], vr[NG][NV];
+        float sc[NT];                                                      // lanes 0 .. 31: the scale of key lane's K of a tile, 32 .. 63: of key lane - 32's V
+        int32_t id[NG];                                                    // pages of the trip that is fetched next; -1: none
+        int64_t k_at[NG], v_at[NG];                                        // ... and byte offsets of this lane's keys (UNIFORM: of the 16 keys' first)
+        uint32_t named[NG];                                                // bit i: a page is named for key i of the 16 (of the trip in kr, vr)
+        const int32_t kl = UNIFORM ? (int32_t)(c16 * g.k_ss) * ES : 0, vl = UNIFORM ? (int32_t)(c16 * g.v_ss) * ES : 0;     // (UNIFORM: they fit)
         auto find = [&](int t) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) id[u] = page_at(pages, divide((uint32_t)(t * kFewKeys + 16 * u + c16), g.page), g.width, g.pages);
-        };
-        auto fetch = [&](int t) {
-            int64_t page[2], at[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int32_t key = t * kFewKeys + 16 * u + c16;
-                named[u] = id[u] >= 0;
-                inside[u] = key >= keys.lo && key < keys.hi;
-                page[u] = named[u] ? id[u] : 0;
-                at[u] = (uint32_t)key - divide((uint32_t)key, g.page) * g.page.d;
-                const char *kp = Kh + (page[u] * g.k_sp + at[u] * g.k_ss) * ES, *vp = Vh + (page[u] * g.v_sp + at[u] * g.v_ss) * ES;
-#pragma unroll
-                for (int n = 0; n < NV; ++n) {
-                    const int d = KIND == CACHE_SAME ? 32 * n + 8 * g4 : 64 * n + 16 * g4;
-                    kr[u][n] = vr[u][n] = u32x4{0, 0, 0, 0};
-                    if (d + 16 / ES <= g.D) {
-                        __builtin_memcpy(&kr[u][n], kp + d * ES, 16);
-                        __builtin_memcpy(&vr[u][n], vp + d * ES, 16);
-                    } else if (KIND != CACHE_SAME && d < g.D) {             // (a head size is a multiple of 8)
-                        __builtin_memcpy(&kr[u][n], kp + d, 8);
-                        __builtin_memcpy(&vr[u][n], vp + d, 8);
-                    }
+            for (int u = 0; u < NG; ++u) {
+                const uint32_t key = (uint32_t)t * TRIP + 16 * u + (UNIFORM ? 0 : c16), index = divide(key, g.page);
+                if constexpr (UNIFORM) {
+                    int32_t p = -1;
+                    if (index < (uint32_t)g.width) p = ((ScalarTable)pages)[index];
+                    id[u] = (uint32_t)p < (uint32_t)g.pages ? p : -1;
+                } else {
+                    id[u] = page_at(pages, index, g.width, g.pages);
                 }
             }
+        };
+        auto locate = [&](int t, uint32_t (&has)[NG]) {
+#pragma unroll
+            for (int u = 0; u < NG; ++u) {
+                const uint32_t key = (uint32_t)t * TRIP + 16 * u + (UNIFORM ? 0 : c16), at = key - divide(key, g.page) * g.page.d;
+                const uint32_t page = id[u] >= 0 ? id[u] : 0;
+                has[u] = UNIFORM ? (id[u] >= 0 ? 0xffffu : 0u) : (uint32_t)__ballot(id[u] >= 0) & 0xffffu;
+                k_at[u] = (times(page, g.k_sp) + times(at, g.k_ss)) * ES;
+                v_at[u] = (times(page, g.v_sp) + times(at, g.v_ss)) * ES;
+            }
             if constexpr (KIND != CACHE_SAME) {
-                const int64_t p = (lane & 16) ? page[1] : page[0], a = (lane & 16) ? at[1] : at[0];
-                sc = lane < 32 ? g.KS[p * g.ks_sp + a * g.ks_ss + (int64_t)h * g.ks_sh] : g.VS[p * g.vs_sp + a * g.vs_ss + (int64_t)h * g.vs_sh];
+#pragma unroll
+                for (int s = 0; s < NT; ++s) {
+                    const uint32_t key = (uint32_t)t * TRIP + 32 * s + (lane & 31), at = key - divide(key, g.page) * g.page.d;
+                    const int32_t p = (lane & 16) ? id[2 * s + 1] : id[2 * s];
+                    const uint32_t page = p >= 0 ? p : 0;
+                    sc[s] = lane < 32 ? KSh[times(page, g.ks_sp) + times(at, g.ks_ss)] : VSh[times(page, g.vs_sp) + times(at, g.vs_ss)];
+                }
             }
         };
+        auto load_rows = [&](u32x4 (&to)[NV], const char *p, int32_t lane_off) {
+            if (KIND == CACHE_SAME || full) {
+#pragma unroll
+                for (int n = 0; n < NV; ++n) __builtin_memcpy(&to[n], p + (uint32_t)(lane_off + doff[n] * ES), 16);
+            } else {
+#pragma unroll
+                for (int n = 0; n < NV; ++n) {
+                    u32x2 lo, hi;
+                    __builtin_memcpy(&lo, p + (uint32_t)(lane_off + doff[n]), 8);
+                    __builtin_memcpy(&hi, p + (uint32_t)(lane_off + doff2[KIND == CACHE_SAME ? 0 : n]), 8);
+                    to[n] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                }
+            }
+        };
+        auto load_k = [&] {
+#pragma unroll
+            for (int u = 0; u < NG; ++u) load_rows(kr[u], Kh + k_at[u], kl);
+        };
+        auto load_v = [&](int u) { load_rows(vr[u], Vh + v_at[u], vl); };
 
-        const int t_end = (keys.hi + kFewKeys - 1) / kFewKeys;
-        int t = keys.lo / kFewKeys + wave;
-        if (keys.lo == keys.hi) t = t_end;
+        const int t_end = keys.lo < keys.hi ? (keys.hi + TRIP - 1) / TRIP : 0;
+        int t = keys.lo / TRIP + wave;
         if (t < t_end) {
             find(t);
-            fetch(t);
+            locate(t, named);
+            load_k();
+#pragma unroll
+            for (int u = 0; u < NG; ++u) load_v(u);
             find(t + kFewWaves);
         }
         for (; t < t_end; t += kFewWaves) {
-            // ---- keys that no page is named for read as NaN: a row that sees one shows it.  V's are zeros, as are those of keys outside the range: what lies
-            // there may be anything, and a weight of 0 does not silence an infinity.
-            if (!__all(named[0] && named[1] && inside[0] && inside[1])) {
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const bool good = named[u] && inside[u];
-#pragma unroll
-                    for (int n = 0; n < NV; ++n) vr[u][n] = good ? vr[u][n] : u32x4{0, 0, 0, 0};
-                }
-            }
+            const int base = t * TRIP, next = t + kFewWaves;
+            const bool more = next < t_end;
             // ---- S^T: lane (c16, g4) gets query c16, keys 16 u + 4 g4 + 0 .. 3
-            float4v st[MB][2];
+            float4v st[MB][NG];
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) st[mb][u] = float4v{0.f, 0.f, 0.f, 0.f};
-            const bool all_named = __all(named[0] && named[1]);
+                for (int u = 0; u < NG; ++u) st[mb][u] = float4v{0.f, 0.f, 0.f, 0.f};
+            if (!full) {                                                   // (Q has zeros there, but 0 * infinity is NaN)
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+                for (int u = 0; u < NG; ++u)
+#pragma unroll
+                    for (int n = 0; n < NV; ++n) {
+                        if constexpr (KIND == CACHE_SAME) {
+                            kr[u][n] = 32 * n + 8 * g4 < g.D ? kr[u][n] : u32x4{0, 0, 0, 0};
+                        } else {
+                            const bool lo = 64 * n + 16 * g4 < g.D, hi = 64 * n + 16 * g4 + 8 < g.D;
+                            kr[u][n] = u32x4{lo ? kr[u][n][0] : 0u, lo ? kr[u][n][1] : 0u, hi ? kr[u][n][2] : 0u, hi ? kr[u][n][3] : 0u};
+                        }
+                    }
+            }
+#pragma unroll
+            for (int u = 0; u < NG; ++u)
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks) {
                     u32x4 kf;
@@ -155,148 +204,199 @@ __global__ __launch_bounds__(64 * kFewWaves, SIZE * MB <= 128 ? 2 : 1) void page
                         const u32x4 raw = kr[u][ks >> 1];
                         kf = widen8<BF16, KIND>((ks & 1) ? u32x2{raw[2], raw[3]} : u32x2{raw[0], raw[1]});
                     }
-                    if (!all_named) kf = named[u] ? kf : u32x4{kNanPair, kNanPair, kNanPair, kNanPair};
 #pragma unroll
                     for (int mb = 0; mb < MB; ++mb) st[mb][u] = mfma16<BF16>(kf, qf[mb][ks], st[mb][u]);
                 }
-            // ---- V and the scales into LDS
-            bool odd = false;                                              // (an infinity or NaN among this lane's values)
-            const int base = t * kFewKeys;
-            bool clear = true;                                             // every row sees every key of the tile
-#pragma unroll
-            for (int mb = 0; mb < MB; ++mb) clear = clear && row_lo[mb] <= base && base + kFewKeys <= row_hi[mb];
-            clear = __all(clear);
-            wavefront_fence();                                             // (the reads of the tile before are done)
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int n = 0; n < NV; ++n) {
-                    const uint32_t row = 16 * u + c16;
-                    if constexpr (KIND == CACHE_SAME) {
-                        if (!clear) odd = odd || any_not_finite<BF16>(vr[u][n]);
-                        lds_write16(vt, lds_at<SIZE>(row, 4 * n + g4), vr[u][n]);
-                    } else {
-                        const u32x4 lo = widen8<BF16, KIND>(u32x2{vr[u][n][0], vr[u][n][1]}), hi = widen8<BF16, KIND>(u32x2{vr[u][n][2], vr[u][n][3]});
-                        if (!clear) odd = odd || any_not_finite<BF16>(lo) || any_not_finite<BF16>(hi);
-                        lds_write16(vt, lds_at<SIZE>(row, 8 * n + 2 * g4), lo);
-                        lds_write16(vt, lds_at<SIZE>(row, 8 * n + 2 * g4 + 1), hi);
-                    }
-                }
             if constexpr (KIND != CACHE_SAME) {
-                scales[wave][lane] = sc;
+                wavefront_fence();                                         // (the reads of the trip before are done)
+#pragma unroll
+                for (int s = 0; s < NT; ++s) scales[wave][(lane < 32 ? 0 : TRIP) + 32 * s + (lane & 31)] = sc[s];
+                wavefront_fence();
             }
-            const bool careful = !clear && __any(odd);
-            wavefront_fence();
-            const int next = t + kFewWaves;
-            if (next < t_end) {
-                fetch(next);
+            // ---- the next trip's K, into registers that are free now
+            uint32_t named_next[NG];
+            if (more) {
+                locate(next, named_next);
+                load_k();
                 find(next + kFewWaves);
+            }
+            // ---- keys that no page is named for have the score NaN: a row that sees one shows it.  V's rows are zeros there, and for keys outside the range: what
+            // lies there may be anything, and a weight of 0 does not silence an infinity.
+            uint32_t good[NG], all = 0xffffu;
+            bool clear = true;                                             // every row sees every key of the trip
+#pragma unroll
+            for (int u = 0; u < NG; ++u) {
+                const int32_t from = keys.lo - base - 16 * u, to = keys.hi - base - 16 * u;        // the range, from the first of the 16 on
+                const uint32_t below = from <= 0 ? 0u : from >= 16 ? 0xffffu : (1u << from) - 1, under = to <= 0 ? 0u : to >= 16 ? 0xffffu : (1u << to) - 1;
+                good[u] = named[u] & under & ~below;
+                all &= good[u];
+            }
+#pragma unroll
+            for (int mb = 0; mb < MB; ++mb) clear = clear && row_lo[mb] <= base && base + TRIP <= row_hi[mb];
+            clear = __all(clear);
+            bool careful = false;
+            if (all != 0xffffu || !clear) {                                // wavefront-uniform
+                bool odd = false;                                          // (an infinity or NaN among this lane's values)
+#pragma unroll
+                for (int u = 0; u < NG; ++u)
+#pragma unroll
+                    for (int n = 0; n < NV; ++n) {
+                        vr[u][n] = (good[u] >> c16) & 1 ? vr[u][n] : u32x4{0, 0, 0, 0};
+                        if constexpr (KIND == CACHE_SAME)
+                            odd = odd || any_not_finite<BF16>(vr[u][n]);
+                        else if constexpr (KIND == CACHE_E4M3)             // (0x7f, the type's one NaN)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const uint32_t x = vr[u][n][i] & 0x7f7f7f7fu;
+                                odd = odd || ((x + 0x01010101u) & 0x80808080u) != 0;
+                            }
+                    }
+                careful = !clear && __any(odd);
             }
 
             // ---- weights
-            u32x4 pk[MB];
+            u32x4 pk[MB][NT];
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) {
-                float s[8];
+                float s[4 * NG];
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
+                for (int u = 0; u < NG; ++u)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) s[4 * u + v] = st[mb][u][v] * g.scale_log2e;
                 if constexpr (KIND != CACHE_SAME) {
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
+                    for (int u = 0; u < NG; ++u) {
                         const float4v k4 = *reinterpret_cast<const float4v *>(&scales[wave][16 * u + 4 * g4]);
 #pragma unroll
                         for (int v = 0; v < 4; ++v) s[4 * u + v] *= k4[v];
                     }
                 }
-                if (!clear) {
+                if (all != 0xffffu || !clear) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int32_t key = base + 16 * (j >> 2) + 4 * g4 + (j & 3);
-                        s[j] = key >= row_lo[mb] && key < row_hi[mb] ? s[j] : -INFINITY;     // (shares begin and end between tiles)
-                    }
+                    for (int u = 0; u < NG; ++u)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            const int32_t key = base + 16 * u + 4 * g4 + v;
+                            const float x = (named[u] >> (4 * g4 + v)) & 1 ? s[4 * u + v] : __builtin_nanf("");
+                            s[4 * u + v] = key >= row_lo[mb] && key < row_hi[mb] ? x : -INFINITY;        // (shares begin and end between trips)
+                        }
                 }
                 float top = s[0];
 #pragma unroll
-                for (int j = 1; j < 8; ++j) top = fmaxf(top, s[j]);
+                for (int j = 1; j < 4 * NG; ++j) top = fmaxf(top, s[j]);
                 top = fmaxf(top, __shfl_xor(top, 16, 64));
                 top = fmaxf(top, __shfl_xor(top, 32, 64));
                 const float m_new = fmaxf(m[mb], top), ref = m_new == -INFINITY ? 0.f : m_new;
                 const float alpha = __builtin_amdgcn_exp2f(m[mb] - ref);
                 m[mb] = m_new;
-                float p[8], sum = 0.f;
+                float p[4 * NG], sum = 0.f;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
+                for (int j = 0; j < 4 * NG; ++j) {
                     p[j] = __builtin_amdgcn_exp2f(s[j] - ref);
                     sum += p[j];
                 }
                 l[mb] = __builtin_fmaf(l[mb], alpha, sum);
+                float shrink = alpha;
                 if constexpr (NORM) {
                     float most = 0.f;                                      // the largest scale that the row sees (fmax passes over NaN)
 #pragma unroll
-                    for (int u = 0; u < 2; ++u)
+                    for (int u = 0; u < NG; ++u) {
+                        const float4v v4 = *reinterpret_cast<const float4v *>(&scales[wave][TRIP + 16 * u + 4 * g4]);
 #pragma unroll
-                        for (int v = 0; v < 4; ++v)
-                            if (s[4 * u + v] != -INFINITY) most = fmaxf(most, __builtin_fabsf(scales[wave][kFewKeys + 16 * u + 4 * g4 + v]));
+                        for (int v = 0; v < 4; ++v) most = fmaxf(most, clear || s[4 * u + v] != -INFINITY ? __builtin_fabsf(v4[v]) : 0.f);
+                    }
                     most = fmaxf(most, __shfl_xor(most, 16, 64));
                     most = fmaxf(most, __shfl_xor(most, 32, 64));
-                    if (__any(most > unit[mb])) {
-                        const float grown = most > unit[mb] ? unit_above(most) : unit[mb], shrink = unit[mb] == 0.f ? 0.f : unit[mb] / grown;
+                    const float grown = most > unit[mb] ? unit_above(most) : unit[mb];
+                    if (grown != unit[mb]) {
+                        shrink *= unit[mb] == 0.f ? 0.f : unit[mb] / grown;
                         unit[mb] = grown;
-                        per_unit[mb] = grown == 0.f ? 0.f : 1.f / grown;
-#pragma unroll
-                        for (int db = 0; db < SIZE / 16; ++db) acc[mb][db] = acc[mb][db] * shrink;
+                        per_unit[mb] = 1.f / grown;
                     }
                 }
-                if (!__all(alpha == 1.f)) {
+                if (!__all(shrink == 1.f)) {
 #pragma unroll
-                    for (int db = 0; db < SIZE / 16; ++db) acc[mb][db] = acc[mb][db] * alpha;
+                    for (int db = 0; db < SIZE / 16; ++db) acc[mb][db] = acc[mb][db] * shrink;
                 }
                 if constexpr (KIND != CACHE_SAME) {
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const float4v v4 = *reinterpret_cast<const float4v *>(&scales[wave][kFewKeys + 16 * u + 4 * g4]);
+                    for (int u = 0; u < NG; ++u) {
+                        const float4v v4 = *reinterpret_cast<const float4v *>(&scales[wave][TRIP + 16 * u + 4 * g4]);
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) {
-                            const float x = p[4 * u + v] * (NORM ? v4[v] * per_unit[mb] : v4[v]);
-                            p[4 * u + v] = s[4 * u + v] == -INFINITY ? 0.f : x;        // (the scale of a hidden key may be anything)
-                        }
+                        for (int v = 0; v < 4; ++v) p[4 * u + v] *= NORM ? v4[v] * per_unit[mb] : v4[v];
+                    }
+                    if (!clear) {                                          // (the scale of a hidden key may be anything)
+#pragma unroll
+                        for (int j = 0; j < 4 * NG; ++j) p[j] = s[j] == -INFINITY ? 0.f : p[j];
                     }
                 }
-                pk[mb] = u32x4{pack_two<BF16>(p[0], p[1]), pack_two<BF16>(p[2], p[3]), pack_two<BF16>(p[4], p[5]), pack_two<BF16>(p[6], p[7])};
-            }
-            // ---- O^T += V^T P^T: lane (c16, g4) supplies d = 16 db + c16 and keys 4 g4 + 0 .. 3, 16 + 4 g4 + 0 .. 3; lane i of a group of 16 points the
-            // transposing read at key i / 4 of its four, 8 bytes i % 4 of the 32
 #pragma unroll
-            for (int db = 0; db < SIZE / 16; ++db) {
-                const uint32_t row = 4 * g4 + (c16 >> 2), chunk = 2 * db + ((c16 >> 1) & 1), half = (c16 & 1) * 8;
-                u32x2 a = lds_read_transposed(vt, lds_at<SIZE>(row, chunk) + half), c = lds_read_transposed(vt, lds_at<SIZE>(row + 16, chunk) + half);
-                if (careful) {
-                    a = u32x2{without_not_finite<BF16>(a[0]), without_not_finite<BF16>(a[1])};
-                    c = u32x2{without_not_finite<BF16>(c[0]), without_not_finite<BF16>(c[1])};
+                for (int i = 0; i < NT; ++i)
+                    pk[mb][i] = u32x4{pack_two<BF16>(p[8 * i], p[8 * i + 1]), pack_two<BF16>(p[8 * i + 2], p[8 * i + 3]), pack_two<BF16>(p[8 * i + 4], p[8 * i + 5]),
+                                      pack_two<BF16>(p[8 * i + 6], p[8 * i + 7])};
+            }
+            // ---- O^T += V^T P^T, 32 keys at a time: V into LDS (its registers take the next trip's), then lane (c16, g4) supplies d = 16 db + c16 and keys
+            // 4 g4 + 0 .. 3, 16 + 4 g4 + 0 .. 3; lane i of a group of 16 points the transposing read at key i / 4 of its four, 8 bytes i % 4 of the 32
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                wavefront_fence();                                         // (the reads of the tile before are done)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                    for (int n = 0; n < NV; ++n) {
+                        const uint32_t row = 16 * u + c16;
+                        const u32x4 x = vr[2 * i + u][n];
+                        if constexpr (KIND == CACHE_SAME) {
+                            lds_write16(vt, lds_at<SIZE>(row, 4 * n + g4), x);
+                        } else {
+                            lds_write16(vt, lds_at<SIZE>(row, 8 * n + 2 * g4), widen8<BF16, KIND>(u32x2{x[0], x[1]}));
+                            lds_write16(vt, lds_at<SIZE>(row, 8 * n + 2 * g4 + 1), widen8<BF16, KIND>(u32x2{x[2], x[3]}));
+                        }
+                    }
+                    if (more) load_v(2 * i + u);
                 }
-#pragma unroll
-                for (int mb = 0; mb < MB; ++mb) acc[mb][db] = mfma16<BF16>(u32x4{a[0], a[1], c[0], c[1]}, pk[mb], acc[mb][db]);
-            }
-            if (careful) {
-                // infinities and NaN of keys that only some rows see: added to those rows alone
-#pragma unroll 1
-                for (int key = 0; key < kFewKeys; ++key)
+                wavefront_fence();
+                const uint32_t row = 4 * g4 + (c16 >> 2), half = (c16 & 1) * 8;
+                auto product = [&](auto clean) {
 #pragma unroll
                     for (int db = 0; db < SIZE / 16; ++db) {
-                        u32x2 v;
-                        __builtin_memcpy(&v, vt + lds_at<SIZE>(key, 2 * db + (g4 >> 1)) + (g4 & 1) * 8, 8);
+                        const uint32_t chunk = 2 * db + ((c16 >> 1) & 1);
+                        u32x2 a = lds_read_transposed(vt, lds_at<SIZE>(row, chunk) + half), c = lds_read_transposed(vt, lds_at<SIZE>(row + 16, chunk) + half);
+                        if constexpr (decltype(clean)::value) {
+                            a = u32x2{without_not_finite<BF16>(a[0]), without_not_finite<BF16>(a[1])};
+                            c = u32x2{without_not_finite<BF16>(c[0]), without_not_finite<BF16>(c[1])};
+                        }
 #pragma unroll
-                        for (int mb = 0; mb < MB; ++mb) {
-                            const bool sees = base + key >= row_lo[mb] && base + key < row_hi[mb];
+                        for (int mb = 0; mb < MB; ++mb) acc[mb][db] = mfma16<BF16>(u32x4{a[0], a[1], c[0], c[1]}, pk[mb][i], acc[mb][db]);
+                    }
+                };
+                if (!careful) {
+                    product(std::false_type{});
+                } else {
+                    product(std::true_type{});
+                    // infinities and NaN of keys that only some rows see: added to those rows alone
+#pragma unroll 1
+                    for (int j = 0; j < 32; ++j)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float x = only_not_finite(widen_one<BF16>(v[e >> 1], e & 1));
-                                acc[mb][db][e] += sees ? x : 0.f;
+                        for (int db = 0; db < SIZE / 16; ++db) {
+                            u32x2 v;
+                            __builtin_memcpy(&v, vt + lds_at<SIZE>(j, 2 * db + (g4 >> 1)) + (g4 & 1) * 8, 8);
+                            const int32_t key = base + 32 * i + j;
+#pragma unroll
+                            for (int mb = 0; mb < MB; ++mb) {
+                                const bool sees = key >= row_lo[mb] && key < row_hi[mb];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) {
+                                    const float x = only_not_finite(widen_one<BF16>(v[e >> 1], e & 1));
+                                    acc[mb][db][e] += sees ? x : 0.f;
+                                }
                             }
                         }
-                    }
+                }
+            }
+            if (more) {
+#pragma unroll
+                for (int u = 0; u < NG; ++u) named[u] = named_next[u];
             }
         }
 

@@ -21,9 +21,15 @@ template <int SIZE, bool BF16, int KIND>
 static nt_status launch_paged_kind(const PagedArgs &a, int rows, int64_t programs, hipStream_t s)
 {
     static_assert(kFewWaves == 4 && kManyWaves == 4, "256 threads");
-    static DeviceOnce few1, few2, many;
-    if (rows == 16) return launch_paged_inst(paged_few_kernel<BF16, KIND, SIZE, 1>, few1, "paged_few_kernel", few_lds(SIZE, 1), a, programs, s);
-    if (rows == 32) return launch_paged_inst(paged_few_kernel<BF16, KIND, SIZE, 2>, few2, "paged_few_kernel", few_lds(SIZE, 2), a, programs, s);
+    static DeviceOnce few1, few2, few1u, few2u, many;
+    if (rows == 16) {
+        if (a.uniform) return launch_paged_inst(paged_few_kernel<BF16, KIND, SIZE, 1, true>, few1u, "paged_few_kernel", few_lds(SIZE, 1), a, programs, s);
+        return launch_paged_inst(paged_few_kernel<BF16, KIND, SIZE, 1, false>, few1, "paged_few_kernel", few_lds(SIZE, 1), a, programs, s);
+    }
+    if (rows == 32) {
+        if (a.uniform) return launch_paged_inst(paged_few_kernel<BF16, KIND, SIZE, 2, true>, few2u, "paged_few_kernel", few_lds(SIZE, 2), a, programs, s);
+        return launch_paged_inst(paged_few_kernel<BF16, KIND, SIZE, 2, false>, few2, "paged_few_kernel", few_lds(SIZE, 2), a, programs, s);
+    }
     return launch_paged_inst(paged_many_kernel<BF16, KIND, SIZE>, many, "paged_many_kernel", many_lds(SIZE), a, programs, s);
 }
 
