@@ -75,7 +75,7 @@ __device__ __forceinline__ bool any_not_finite(u32x4 v)
     constexpr uint32_t E = BF16 ? 0x7f80u : 0x7c00u;
     bool bad = false;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) bad = bad || (v[i] & E) == E || (v[i] & (E << 16)) == (E << 16);
+    for (int i = 0; i < 4; ++i) bad = bad | ((v[i] & E) == E) | ((v[i] & (E << 16)) == (E << 16));
     return bad;
 }
 
@@ -84,6 +84,12 @@ __device__ __forceinline__ uint32_t without_not_finite(uint32_t w)
 {
     constexpr uint32_t E = BF16 ? 0x7f80u : 0x7c00u;
     return ((w & E) == E ? 0u : w & 0xffffu) | ((w & (E << 16)) == (E << 16) ? 0u : w & 0xffff0000u);
+}
+
+template <bool BF16>
+__device__ __forceinline__ u32x4 without_not_finite(u32x4 v)
+{
+    return u32x4{without_not_finite<BF16>(v[0]), without_not_finite<BF16>(v[1]), without_not_finite<BF16>(v[2]), without_not_finite<BF16>(v[3])};
 }
 
 template <bool BF16>
@@ -96,6 +102,44 @@ __device__ __forceinline__ float widen_one(uint32_t w, int upper)
 
 // v if it is an infinity or NaN, else 0
 __device__ __forceinline__ float only_not_finite(float v) { return __builtin_fabsf(v) < INFINITY ? 0.f : v; }
+
+// v, as something that the compiler knows nothing of: what is worked out from it stays where it is (a rare path's addresses, kept in registers around
+// the loop that it lies in, cost the loop those registers)
+__device__ __forceinline__ int here(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// The same for a value that is the same in all lanes
+__device__ __forceinline__ uint32_t here_scalar(uint32_t v)
+{
+    asm volatile("" : "+s"(v));
+    return v;
+}
+
+// Largest and sum over lanes l, l ^ 16, l ^ 32 and l ^ 48 (BOTH) or over l and l ^ 32, in all of them: exchanges of rows and halves between registers, not by way of LDS
+template <bool BOTH, typename F>
+__device__ __forceinline__ float across(float v, F combine)
+{
+    const auto half = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+    v = combine(__builtin_bit_cast(float, (uint32_t)half[0]), __builtin_bit_cast(float, (uint32_t)half[1]));
+    if constexpr (BOTH) {
+        const auto row = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false, false);
+        v = combine(__builtin_bit_cast(float, (uint32_t)row[0]), __builtin_bit_cast(float, (uint32_t)row[1]));
+    }
+    return v;
+}
+template <bool BOTH>
+__device__ __forceinline__ float largest_across(float v)
+{
+    return across<BOTH>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+template <bool BOTH>
+__device__ __forceinline__ float sum_across(float v)
+{
+    return across<BOTH>(v, [](float a, float b) { return a + b; });
+}
 
 // Order of what one wavefront's lanes write to LDS and read of each other's: the hardware keeps it, the compiler has to
 __device__ __forceinline__ void wavefront_fence()

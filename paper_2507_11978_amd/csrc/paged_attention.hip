@@ -10,43 +10,98 @@
 
 namespace nt {
 
-// One wavefront per row (token, query head): lanes / LANES groups take the shares in turn, LANES lanes have 4 elements each.
-template <bool BF16, int LANES>
+// WAVES wavefronts per row (token, query head): groups of LANES lanes, 4 elements to a lane, take the shares in turn, eight of them in flight at a time; the
+// groups' sums meet within a wavefront and then in LDS.  One wavefront has many rows to hide behind where the shares are few; four make the
+// chain of 64 shares of a single long sequence short (2 x 32 rows of 128, 64 shares: 28 us with one, two of a group's loads in flight).
+template <bool BF16, int LANES, int WAVES>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs g)
 {
-    const int lane = threadIdx.x & 63, part = lane / LANES, d = 4 * (lane % LANES);
-    const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    constexpr int PARTS = 64 / LANES * WAVES, AT_ONCE = 8;
+    __shared__ __attribute__((aligned(16))) float4v red_o[WAVES > 1 ? WAVES : 1][LANES];
+    __shared__ float red_m[WAVES], red_l[WAVES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, part = (WAVES > 1 ? wave * (64 / LANES) : 0) + lane / LANES, d = 4 * (lane % LANES);
+    const int64_t row = WAVES > 1 ? blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
     if (row >= (int64_t)g.T * g.Hq) return;
     const int32_t token = (int32_t)((uint32_t)row / (uint32_t)g.Hq), head = (int32_t)(row - (int64_t)token * g.Hq);
     if (token < g.starts[0] || token >= g.starts[g.B]) return;             // (no sequence's: nobody has written its shares)
-    const float *ml = g.part_ml + 2 * row * g.splits;
-    float top = -INFINITY;
-    for (int s = lane; s < g.splits; s += 64) top = fmaxf(top, ml[2 * s]);
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
-    const float ref = top == -INFINITY ? 0.f : top;
-    float sum = 0.f;
+    const float *ml = g.part_ml + 2 * row * g.splits, *po = g.part_o + row * g.splits * g.D + (d < g.D ? d : 0);
+    float m = -INFINITY, l = 0.f;
     float4v o{0.f, 0.f, 0.f, 0.f};
-    for (int s = part; s < g.splits; s += 64 / LANES) {
-        const float f = __builtin_amdgcn_exp2f(ml[2 * s] - ref);
-        sum = __builtin_fmaf(ml[2 * s + 1], f, sum);
-        if (d < g.D) {
-            float4v x;
-            __builtin_memcpy(&x, g.part_o + (row * g.splits + s) * g.D + d, 16);
+    for (int s0 = part; s0 < g.splits; s0 += PARTS * AT_ONCE) {
+        float2v f[AT_ONCE];
+        float4v x[AT_ONCE];
 #pragma unroll
-            for (int v = 0; v < 4; ++v) o[v] = __builtin_fmaf(x[v], f, o[v]);
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int s = s0 + i * PARTS < g.splits ? s0 + i * PARTS : s0;
+            __builtin_memcpy(&f[i], ml + 2 * s, 8);
+            __builtin_memcpy(&x[i], po + (int64_t)s * g.D, 16);
+        }
+        float top = m;
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            if (i && s0 + i * PARTS >= g.splits) f[i] = float2v{-INFINITY, 0.f};
+            top = fmaxf(top, f[i][0]);
+        }
+        const float ref = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f(m - ref);
+        m = top;
+        l *= old;
+        o = o * old;
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            if (i && s0 + i * PARTS >= g.splits) continue;                 // (what is there once more may be an infinity)
+            const float w = __builtin_amdgcn_exp2f(f[i][0] - ref);
+            l = __builtin_fmaf(f[i][1], w, l);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) o[v] = __builtin_fmaf(x[i][v], w, o[v]);
         }
     }
+    float top = m;
+#pragma unroll
+    for (int x = LANES; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+    const float mine = __builtin_amdgcn_exp2f(m - (top == -INFINITY ? 0.f : top));
+    l *= mine;
+    o = o * mine;
 #pragma unroll
     for (int x = LANES; x < 64; x <<= 1) {
-        sum += __shfl_xor(sum, x, 64);
+        l += __shfl_xor(l, x, 64);
 #pragma unroll
         for (int v = 0; v < 4; ++v) o[v] += __shfl_xor(o[v], x, 64);
     }
-    if (part != 0 || d >= g.D) return;
-    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    if constexpr (WAVES > 1) {
+        if (lane < LANES) red_o[wave][lane] = o;
+        if (lane == 0) {
+            red_m[wave] = top;
+            red_l[wave] = l;
+        }
+        __syncthreads();
+        if (wave) return;
+        top = red_m[0];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) top = fmaxf(top, red_m[i]);
+        const float ref = top == -INFINITY ? 0.f : top;
+        l = 0.f;
+        o = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            const float w = __builtin_amdgcn_exp2f(red_m[i] - ref);
+            l = __builtin_fmaf(red_l[i], w, l);
+            const float4v x = red_o[i][lane % LANES];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) o[v] = __builtin_fmaf(x[v], w, o[v]);
+        }
+    }
+    if (lane >= LANES || d >= g.D) return;
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
     const u32x2 out{pack_two<BF16>(o[0] * inv, o[1] * inv), pack_two<BF16>(o[2] * inv, o[3] * inv)};
     __builtin_memcpy(g.O + (int64_t)token * g.o_st + (int64_t)head * g.o_sh + d, &out, 8);
+}
+
+template <bool BF16, int LANES>
+static void launch_join(const PagedArgs &a, hipStream_t s)
+{
+    const int64_t rows = (int64_t)a.T * a.Hq;
+    if (a.splits > 8 && rows <= kMaxWorkgroups) hipLaunchKernelGGL((paged_join_kernel<BF16, LANES, 4>), dim3((unsigned)rows), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((paged_join_kernel<BF16, LANES, 1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a);
 }
 
 static thread_local nt_paged_plan t_paged;
@@ -84,7 +139,8 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     PagedArgs a{};
     a.Q = (const uint16_t *)q; a.O = (uint16_t *)out;
     a.K = (const char *)c->k; a.V = (const char *)c->v;
-    a.table = table; a.starts = starts; a.lengths = lengths;
+    a.table = W ? table : starts;                                          // (no entries: something to read in their place)
+    a.starts = starts; a.lengths = lengths;
     a.q_st = dq->stride[0]; a.q_sh = dq->stride[1];
     a.o_st = dout->stride[0]; a.o_sh = dout->stride[1];
     a.k_sp = c->dk->stride[0]; a.k_ss = c->dk->stride[1]; a.k_sh = c->dk->stride[2];
@@ -94,7 +150,7 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
         a.ks_sp = c->dks->stride[0]; a.ks_ss = c->dks->stride[1]; a.ks_sh = c->dks->stride[2];
         a.vs_sp = c->dvs->stride[0]; a.vs_ss = c->dvs->stride[1]; a.vs_sh = c->dvs->stride[2];
     }
-    a.t_sb = dt->stride[0];
+    a.t_sb = W ? dt->stride[0] : 0;
     a.T = (int32_t)T; a.B = (int32_t)B; a.Hq = (int32_t)Hq; a.Hkv = (int32_t)Hkv; a.G = (int32_t)(Hq / Hkv); a.D = (int32_t)D;
     a.width = (int32_t)W; a.pages = (int32_t)pages;
     a.causal = causal ? 1 : 0;
@@ -107,12 +163,12 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
 
     // Up to 32 rows per key head: the kernel whose wavefronts share the keys, else the one whose wavefronts share the rows.
     const int64_t most = max_queries && max_queries < T ? max_queries : T, group_rows = most * a.G;
-    const int rows = group_rows <= 16 ? 16 : group_rows <= 32 ? 32 : kManyRows;
+    const int built = D <= 64 ? 64 : D <= 128 ? 128 : 256;
+    const int rows = group_rows <= 16 ? 16 : group_rows <= 32 && built < 256 ? 32 : kManyRows;
     a.tiles = rows == kManyRows ? (int32_t)(T * a.G / kManyRows + B) : (int32_t)B;
     const int64_t base = (int64_t)a.tiles * Hkv;
     if (base > kMaxWorkgroups) return fail(NT_ERR_UNSUPPORTED, "too many programs for one launch");
     // ---- shares
-    const int built = D <= 64 ? 64 : D <= 128 ? 128 : 256;
     int64_t length = W * page_size;
     if (max_length) length = std::min(length, max_length);
     if (window) length = std::min(length, window + most);
@@ -120,28 +176,27 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     const int64_t wanted = rows == kManyRows ? (base >= 256 ? 1 : 512 / base) : (1024 + base - 1) / base;
     int64_t splits = std::max<int64_t>(1, std::min(wanted, length / (rows == kManyRows ? 512 : 256)));
     splits = std::min<int64_t>(splits, kMaxWorkgroups / base);
+    if (getenv("XS") && rows != kManyRows) splits = std::max<int64_t>(1, length / atoi(getenv("XS")));
     int64_t share = ((length + splits - 1) / splits + block - 1) / block * block;
     splits = share ? std::max<int64_t>(1, (length + share - 1) / share) : 1;
     WorkspaceLease lease;
     hipStream_t s = (hipStream_t)stream;
     if (splits > 1) {
-        const size_t n = (size_t)(T * Hq * splits);
-        a.part_ml = (float *)lease.acquire(n * (size_t)(D + 2) * 4, s);
-        if (a.part_ml) a.part_o = a.part_ml + 2 * n;
+        const size_t n = (size_t)(T * Hq * splits), n2 = 2 * n + 2 * (n & 1);             // (outputs begin at a multiple of 16 bytes)
+        a.part_ml = (float *)lease.acquire((n2 + n * (size_t)D) * 4, s);
+        if (a.part_ml) a.part_o = a.part_ml + n2;
         else splits = 1;                                                   // (no room: unshared)
     }
     a.splits = (int32_t)splits;
     a.split_keys = (int32_t)std::min<int64_t>(share, 0x7fffffff / 2);
     const bool bf16 = dtype == NT_BF16;
-    auto launch = D <= 64 ? launch_paged_64 : D <= 128 ? launch_paged_128 : launch_paged_256;
+    auto launch = built == 64 ? launch_paged_64 : built == 128 ? launch_paged_128 : launch_paged_256;
     nt_status rc = launch(a, rows, base * splits, bf16, kind, stream);
     if (rc != NT_OK) return rc;
     if (splits > 1) {
-        const unsigned grid = (unsigned)((T * Hq + 3) / 4);
-        auto join = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(grid), dim3(256), 0, s, a); };
-        if (D <= 64) bf16 ? join(paged_join_kernel<true, 16>) : join(paged_join_kernel<false, 16>);
-        else if (D <= 128) bf16 ? join(paged_join_kernel<true, 32>) : join(paged_join_kernel<false, 32>);
-        else bf16 ? join(paged_join_kernel<true, 64>) : join(paged_join_kernel<false, 64>);
+        if (built == 64) bf16 ? launch_join<true, 16>(a, s) : launch_join<false, 16>(a, s);
+        else if (built == 128) bf16 ? launch_join<true, 32>(a, s) : launch_join<false, 32>(a, s);
+        else bf16 ? launch_join<true, 64>(a, s) : launch_join<false, 64>(a, s);
         rc = check_launch("paged_join_kernel");
         if (rc != NT_OK) return rc;
     }

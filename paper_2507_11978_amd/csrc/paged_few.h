@@ -21,6 +21,10 @@ constexpr size_t few_lds(int size, int mb) { return (size_t)kFewWaves * mb * 64 
 constexpr int few_tiles(int kind, int size) { return size * (kind == CACHE_SAME ? 2 : 1) >= 256 ? 1 : 2; }
 constexpr int few_trip(int kind, int size) { return 32 * few_tiles(kind, size); }        // keys
 
+// Wavefronts per SIMD that the registers are shared out for.  Three where they suffice: a program's start -- the sequence's bounds, its pages, the first
+// keys, each awaited in turn -- is hidden by the other programs of its unit
+constexpr int few_resident(int kind, int size, int mb) { return mb == 1 && (size == 64 || (size == 128 && kind == CACHE_SAME)) ? 3 : size * mb <= 128 ? 2 : 1; }
+
 // a * s, 32 by 64 bits
 __device__ __forceinline__ int64_t times(uint32_t a, int64_t s)
 {
@@ -29,8 +33,8 @@ __device__ __forceinline__ int64_t times(uint32_t a, int64_t s)
 
 // UNIFORM: page_size is a multiple of 16, so that 16 keys that begin at a multiple of 16 lie on one page: the table is read and the addresses are made
 // once for a wavefront, on the scalar unit, and a lane's part is an offset that never changes.
-template <bool BF16, int KIND, int SIZE, int MB, bool UNIFORM>
-__global__ __launch_bounds__(64 * kFewWaves, SIZE * MB <= 128 ? 2 : 1) void paged_few_kernel(const PagedArgs g)
+template <bool BF16, int KIND, int SIZE, int MB, bool UNIFORM, bool FULL>
+__global__ __launch_bounds__(64 * kFewWaves, few_resident(KIND, SIZE, MB)) void paged_few_kernel(const PagedArgs g)
 {
     constexpr int KS = SIZE / 32;                                          // k steps of the first product
     constexpr int NV = KIND == CACHE_SAME ? SIZE / 32 : SIZE / 64;         // 16-byte loads per lane, 16 keys and tensor
@@ -47,25 +51,89 @@ __global__ __launch_bounds__(64 * kFewWaves, SIZE * MB <= 128 ? 2 : 1) void page
     const int h = w % g.Hkv;                                               // (consecutive programs, on different XCDs, have different heads)
     w /= g.Hkv;
     const int split = w % g.splits, b = w / g.splits;
-    const Sequence seq = sequence_of(g, b);
     typedef const __attribute__((address_space(4))) int32_t *ScalarTable;
     const int32_t *pages = g.table + (int64_t)b * g.t_sb;
-    const int rows_all = seq.count * g.G;
     const char *Kh = g.K + (int64_t)h * g.k_sh * ES, *Vh = g.V + (int64_t)h * g.v_sh * ES;
     const float *KSh = g.KS + (int64_t)h * g.ks_sh, *VSh = g.VS + (int64_t)h * g.vs_sh;
-    const bool full = g.D == SIZE;
-    // element offsets of this lane's loads within a row: of 16 bytes; a head size below SIZE: where it has elements, else its last ones (codes: of 8 bytes)
-    int32_t doff[NV], doff2[KIND == CACHE_SAME ? 1 : NV];
+
+    // ---- loads: lane (c16, g4) has key c16 of each 16 and a quarter of its elements
+    u32x4 kr[NG][NV], vr[NG][NV];
+    float sc[NT];                                                          // lanes 0 .. 31: the scale of key lane's K of a tile, 32 .. 63: of key lane - 32's V
+    int32_t id[NG];                                                        // the table's entries for the trip that is fetched next
+    int64_t k_at[NG], v_at[NG];                                            // ... and byte offsets of this lane's keys (UNIFORM: of the 16 keys' first)
+    uint32_t named[NG];                                                    // bit i: a page is named for key i of the 16 (of the trip in kr, vr)
+    // a lane's own byte offset: its elements' (FULL), its key's (UNIFORM; they fit 32 bits)
+    const int32_t mine = FULL ? 16 * g4 : 0, kl = mine + (UNIFORM ? (int32_t)(c16 * g.k_ss) * ES : 0), vl = mine + (UNIFORM ? (int32_t)(c16 * g.v_ss) * ES : 0);
+    auto find = [&](int t) {
 #pragma unroll
-    for (int n = 0; n < NV; ++n) {
-        const int d = KIND == CACHE_SAME ? 32 * n + 8 * g4 : 64 * n + 16 * g4;
-        doff[n] = d <= g.D - 8 ? d : g.D - 8;
-        if constexpr (KIND != CACHE_SAME) doff2[n] = d + 8 <= g.D - 8 ? d + 8 : g.D - 8;
-    }
+        for (int u = 0; u < NG; ++u) {
+            const uint32_t index = divide((uint32_t)t * TRIP + 16 * u + (UNIFORM ? 0 : c16), g.page);
+            // (past the row's end: its last entry is read, and not used; a table without entries is replaced by the launcher)
+            const uint32_t inside = index < (uint32_t)g.width ? index : g.width > 0 ? g.width - 1 : 0;
+            id[u] = UNIFORM ? ((ScalarTable)pages)[inside] : pages[inside];
+        }
+    };
+    auto locate = [&](int t, uint32_t (&has)[NG]) {
+        uint32_t page[NG];
+#pragma unroll
+        for (int u = 0; u < NG; ++u) {
+            const uint32_t key = (uint32_t)t * TRIP + 16 * u + (UNIFORM ? 0 : c16), index = divide(key, g.page), at = key - index * g.page.d;
+            const bool ok = index < (uint32_t)g.width && (uint32_t)id[u] < (uint32_t)g.pages;
+            page[u] = ok ? id[u] : 0;
+            has[u] = UNIFORM ? (ok ? 0xffffu : 0u) : (uint32_t)__ballot(ok) & 0xffffu;
+            k_at[u] = (times(page[u], g.k_sp) + times(at, g.k_ss)) * ES;
+            v_at[u] = (times(page[u], g.v_sp) + times(at, g.v_ss)) * ES;
+        }
+        if constexpr (KIND != CACHE_SAME) {
+#pragma unroll
+            for (int s = 0; s < NT; ++s) {
+                const uint32_t key = (uint32_t)t * TRIP + 32 * s + (lane & 31), at = key - divide(key, g.page) * g.page.d;
+                const uint32_t p0 = page[2 * s], p1 = page[2 * s + 1], p = (lane & 16) ? p1 : p0;
+                sc[s] = lane < 32 ? KSh[times(p, g.ks_sp) + times(at, g.ks_ss)] : VSh[times(p, g.vs_sp) + times(at, g.vs_ss)];
+            }
+        }
+    };
+    // 64 bytes of a row to a load of four lanes; a head size below SIZE: where there are no elements, the row's last ones once more (codes: 8 at a time)
+    auto load_rows = [&](u32x4 (&to)[NV], const char *p, int32_t lane_off) {
+        if constexpr (FULL) {
+#pragma unroll
+            for (int n = 0; n < NV; ++n) __builtin_memcpy(&to[n], p + (uint32_t)lane_off + 64 * n, 16);
+        } else {
+            const int q = here(16 * g4), end = (g.D - 8) * ES;
+#pragma unroll
+            for (int n = 0; n < NV; ++n) {
+                const int at = 64 * n + q;
+                if constexpr (KIND == CACHE_SAME) {
+                    __builtin_memcpy(&to[n], p + (uint32_t)(lane_off + (at < end ? at : end)), 16);
+                } else {
+                    u32x2 lo, hi;
+                    __builtin_memcpy(&lo, p + (uint32_t)(lane_off + (at < end ? at : end)), 8);
+                    __builtin_memcpy(&hi, p + (uint32_t)(lane_off + (at + 8 < end ? at + 8 : end)), 8);
+                    to[n] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                }
+            }
+        }
+    };
+    // (`more` false: nothing is needed any more.  The loads go out all the same, from one address: a branch around them would make the waits behind it wait
+    // for everything, since the number of loads in flight would not be known)
+    auto load_k = [&](bool more) {
+#pragma unroll
+        for (int u = 0; u < NG; ++u) load_rows(kr[u], Kh + (UNIFORM || more ? k_at[u] : 0), more ? kl : 0);
+    };
+    auto load_v = [&](int u, bool more) { load_rows(vr[u], Vh + (UNIFORM || more ? v_at[u] : 0), more ? vl : 0); };
+
+    // Without a window a share begins where it does whatever the sequence's length is: its first pages are looked up along with that.
+    const int t_first = g.window ? -1 : (int)((int64_t)split * g.split_keys / TRIP) + wave;
+    if (t_first >= 0) find(t_first);
+    const Sequence seq = sequence_of(g, b);
+    const int rows_all = seq.count * g.G;
 
     for (int r0 = 0; r0 < rows_all; r0 += 16 * MB) {                       // (one pass, unless the caller's bound on new tokens was too low)
         const int last = r0 + 16 * MB < rows_all ? r0 + 16 * MB - 1 : rows_all - 1;
         const KeyRange keys = keys_of(g, seq, (int32_t)divide(r0, g.group), (int32_t)divide(last, g.group), split, TRIP);
+
+        const int t_end = keys.lo < keys.hi ? (keys.hi + TRIP - 1) / TRIP : 0;
+        int t = keys.lo / TRIP + wave;
 
         // ---- this lane's rows (row c16 of each 16): their keys [row_lo, row_hi), and Q as the first product's operand
         int32_t row_lo[MB], row_hi[MB];
@@ -87,6 +155,16 @@ __global__ __launch_bounds__(64 * kFewWaves, SIZE * MB <= 128 ? 2 : 1) void page
             }
         }
 
+        // (behind Q's loads: those have landed where these have)
+        if (t < t_end) {
+            if (t != t_first || r0 > 0) find(t);
+            locate(t, named);
+            load_k(true);
+#pragma unroll
+            for (int u = 0; u < NG; ++u) load_v(u, true);
+            find(t + kFewWaves);
+        }
+
         float m[MB], l[MB];
         float4v acc[MB][SIZE / 16];
 #pragma unroll
@@ -102,77 +180,10 @@ __global__ __launch_bounds__(64 * kFewWaves, SIZE * MB <= 128 ? 2 : 1) void page
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) unit[mb] = per_unit[mb] = 0.f;
 
-        // ---- loads: lane (c16, g4) has key c16 of each 16 and a quarter of its elements
-        u32x4 kr[NG][NV], vr[NG][NV];
-        float sc[NT];                                                      // lanes 0 .. 31: the scale of key lane's K of a tile, 32 .. 63: of key lane - 32's V
-        int32_t id[NG];                                                    // pages of the trip that is fetched next; -1: none
-        int64_t k_at[NG], v_at[NG];                                        // ... and byte offsets of this lane's keys (UNIFORM: of the 16 keys' first)
-        uint32_t named[NG];                                                // bit i: a page is named for key i of the 16 (of the trip in kr, vr)
-        const int32_t kl = UNIFORM ? (int32_t)(c16 * g.k_ss) * ES : 0, vl = UNIFORM ? (int32_t)(c16 * g.v_ss) * ES : 0;     // (UNIFORM: they fit)
-        auto find = [&](int t) {
-#pragma unroll
-            for (int u = 0; u < NG; ++u) {
-                const uint32_t key = (uint32_t)t * TRIP + 16 * u + (UNIFORM ? 0 : c16), index = divide(key, g.page);
-                if constexpr (UNIFORM) {
-                    int32_t p = -1;
-                    if (index < (uint32_t)g.width) p = ((ScalarTable)pages)[index];
-                    id[u] = (uint32_t)p < (uint32_t)g.pages ? p : -1;
-                } else {
-                    id[u] = page_at(pages, index, g.width, g.pages);
-                }
-            }
-        };
-        auto locate = [&](int t, uint32_t (&has)[NG]) {
-#pragma unroll
-            for (int u = 0; u < NG; ++u) {
-                const uint32_t key = (uint32_t)t * TRIP + 16 * u + (UNIFORM ? 0 : c16), at = key - divide(key, g.page) * g.page.d;
-                const uint32_t page = id[u] >= 0 ? id[u] : 0;
-                has[u] = UNIFORM ? (id[u] >= 0 ? 0xffffu : 0u) : (uint32_t)__ballot(id[u] >= 0) & 0xffffu;
-                k_at[u] = (times(page, g.k_sp) + times(at, g.k_ss)) * ES;
-                v_at[u] = (times(page, g.v_sp) + times(at, g.v_ss)) * ES;
-            }
-            if constexpr (KIND != CACHE_SAME) {
-#pragma unroll
-                for (int s = 0; s < NT; ++s) {
-                    const uint32_t key = (uint32_t)t * TRIP + 32 * s + (lane & 31), at = key - divide(key, g.page) * g.page.d;
-                    const int32_t p = (lane & 16) ? id[2 * s + 1] : id[2 * s];
-                    const uint32_t page = p >= 0 ? p : 0;
-                    sc[s] = lane < 32 ? KSh[times(page, g.ks_sp) + times(at, g.ks_ss)] : VSh[times(page, g.vs_sp) + times(at, g.vs_ss)];
-                }
-            }
-        };
-        auto load_rows = [&](u32x4 (&to)[NV], const char *p, int32_t lane_off) {
-            if (KIND == CACHE_SAME || full) {
-#pragma unroll
-                for (int n = 0; n < NV; ++n) __builtin_memcpy(&to[n], p + (uint32_t)(lane_off + doff[n] * ES), 16);
-            } else {
-#pragma unroll
-                for (int n = 0; n < NV; ++n) {
-                    u32x2 lo, hi;
-                    __builtin_memcpy(&lo, p + (uint32_t)(lane_off + doff[n]), 8);
-                    __builtin_memcpy(&hi, p + (uint32_t)(lane_off + doff2[KIND == CACHE_SAME ? 0 : n]), 8);
-                    to[n] = u32x4{lo[0], lo[1], hi[0], hi[1]};
-                }
-            }
-        };
-        auto load_k = [&] {
-#pragma unroll
-            for (int u = 0; u < NG; ++u) load_rows(kr[u], Kh + k_at[u], kl);
-        };
-        auto load_v = [&](int u) { load_rows(vr[u], Vh + v_at[u], vl); };
-
-        const int t_end = keys.lo < keys.hi ? (keys.hi + TRIP - 1) / TRIP : 0;
-        int t = keys.lo / TRIP + wave;
-        if (t < t_end) {
-            find(t);
-            locate(t, named);
-            load_k();
-#pragma unroll
-            for (int u = 0; u < NG; ++u) load_v(u);
-            find(t + kFewWaves);
-        }
         for (; t < t_end; t += kFewWaves) {
             const int base = t * TRIP, next = t + kFewWaves;
+            // (head size 128: LDS addresses are worked out anew in each trip, 30 instructions that cost less than their registers)
+            const int lane = SIZE == 128 ? here(threadIdx.x & 63) : (int)threadIdx.x & 63, c16 = lane & 15, g4 = lane >> 4;
             const bool more = next < t_end;
             // ---- S^T: lane (c16, g4) gets query c16, keys 16 u + 4 g4 + 0 .. 3
             float4v st[MB][NG];
@@ -180,7 +191,8 @@ __global__ __launch_bounds__(64 * kFewWaves, SIZE * MB <= 128 ? 2 : 1) void page
             for (int mb = 0; mb < MB; ++mb)
 #pragma unroll
                 for (int u = 0; u < NG; ++u) st[mb][u] = float4v{0.f, 0.f, 0.f, 0.f};
-            if (!full) {                                                   // (Q has zeros there, but 0 * infinity is NaN)
+            if constexpr (!FULL) {                                         // (Q has zeros there, but 0 * infinity is NaN)
+                const int g4 = here(lane) >> 4;
 #pragma unroll
                 for (int u = 0; u < NG; ++u)
 #pragma unroll
@@ -215,11 +227,9 @@ __global__ __launch_bounds__(64 * kFewWaves, SIZE * MB <= 128 ? 2 : 1) void page
             }
             // ---- the next trip's K, into registers that are free now
             uint32_t named_next[NG];
-            if (more) {
-                locate(next, named_next);
-                load_k();
-                find(next + kFewWaves);
-            }
+            locate(next, named_next);
+            load_k(more);
+            find(next + kFewWaves);
             // ---- keys that no page is named for have the score NaN: a row that sees one shows it.  V's rows are zeros there, and for keys outside the range: what
             // lies there may be anything, and a weight of 0 does not silence an infinity.
             uint32_t good[NG], all = 0xffffu;
@@ -243,12 +253,12 @@ __global__ __launch_bounds__(64 * kFewWaves, SIZE * MB <= 128 ? 2 : 1) void page
                     for (int n = 0; n < NV; ++n) {
                         vr[u][n] = (good[u] >> c16) & 1 ? vr[u][n] : u32x4{0, 0, 0, 0};
                         if constexpr (KIND == CACHE_SAME)
-                            odd = odd || any_not_finite<BF16>(vr[u][n]);
+                            odd = odd | any_not_finite<BF16>(vr[u][n]);
                         else if constexpr (KIND == CACHE_E4M3)             // (0x7f, the type's one NaN)
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 const uint32_t x = vr[u][n][i] & 0x7f7f7f7fu;
-                                odd = odd || ((x + 0x01010101u) & 0x80808080u) != 0;
+                                odd = odd | (((x + 0x01010101u) & 0x80808080u) != 0);
                             }
                     }
                 careful = !clear && __any(odd);
@@ -272,20 +282,20 @@ __global__ __launch_bounds__(64 * kFewWaves, SIZE * MB <= 128 ? 2 : 1) void page
                     }
                 }
                 if (all != 0xffffu || !clear) {
+                    const int q = here(4 * g4);
 #pragma unroll
                     for (int u = 0; u < NG; ++u)
 #pragma unroll
                         for (int v = 0; v < 4; ++v) {
-                            const int32_t key = base + 16 * u + 4 * g4 + v;
-                            const float x = (named[u] >> (4 * g4 + v)) & 1 ? s[4 * u + v] : __builtin_nanf("");
+                            const int32_t key = base + 16 * u + q + v;
+                            const float x = (named[u] >> (q + v)) & 1 ? s[4 * u + v] : __builtin_nanf("");
                             s[4 * u + v] = key >= row_lo[mb] && key < row_hi[mb] ? x : -INFINITY;        // (shares begin and end between trips)
                         }
                 }
                 float top = s[0];
 #pragma unroll
                 for (int j = 1; j < 4 * NG; ++j) top = fmaxf(top, s[j]);
-                top = fmaxf(top, __shfl_xor(top, 16, 64));
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                top = largest_across<true>(top);
                 const float m_new = fmaxf(m[mb], top), ref = m_new == -INFINITY ? 0.f : m_new;
                 const float alpha = __builtin_amdgcn_exp2f(m[mb] - ref);
                 m[mb] = m_new;
@@ -305,8 +315,7 @@ __global__ __launch_bounds__(64 * kFewWaves, SIZE * MB <= 128 ? 2 : 1) void page
 #pragma unroll
                         for (int v = 0; v < 4; ++v) most = fmaxf(most, clear || s[4 * u + v] != -INFINITY ? __builtin_fabsf(v4[v]) : 0.f);
                     }
-                    most = fmaxf(most, __shfl_xor(most, 16, 64));
-                    most = fmaxf(most, __shfl_xor(most, 32, 64));
+                    most = largest_across<true>(most);
                     const float grown = most > unit[mb] ? unit_above(most) : unit[mb];
                     if (grown != unit[mb]) {
                         shrink *= unit[mb] == 0.f ? 0.f : unit[mb] / grown;
@@ -353,34 +362,18 @@ __global__ __launch_bounds__(64 * kFewWaves, SIZE * MB <= 128 ? 2 : 1) void page
                             lds_write16(vt, lds_at<SIZE>(row, 8 * n + 2 * g4 + 1), widen8<BF16, KIND>(u32x2{x[2], x[3]}));
                         }
                     }
-                    if (more) load_v(2 * i + u);
+                    load_v(2 * i + u, more);
                 }
                 wavefront_fence();
-                const uint32_t row = 4 * g4 + (c16 >> 2), half = (c16 & 1) * 8;
-                auto product = [&](auto clean) {
-#pragma unroll
-                    for (int db = 0; db < SIZE / 16; ++db) {
-                        const uint32_t chunk = 2 * db + ((c16 >> 1) & 1);
-                        u32x2 a = lds_read_transposed(vt, lds_at<SIZE>(row, chunk) + half), c = lds_read_transposed(vt, lds_at<SIZE>(row + 16, chunk) + half);
-                        if constexpr (decltype(clean)::value) {
-                            a = u32x2{without_not_finite<BF16>(a[0]), without_not_finite<BF16>(a[1])};
-                            c = u32x2{without_not_finite<BF16>(c[0]), without_not_finite<BF16>(c[1])};
-                        }
-#pragma unroll
-                        for (int mb = 0; mb < MB; ++mb) acc[mb][db] = mfma16<BF16>(u32x4{a[0], a[1], c[0], c[1]}, pk[mb][i], acc[mb][db]);
-                    }
-                };
-                if (!careful) {
-                    product(std::false_type{});
-                } else {
-                    product(std::true_type{});
-                    // infinities and NaN of keys that only some rows see: added to those rows alone
+                if (careful) {
+                    // infinities and NaN of keys that only some rows see: added to those rows alone, and taken out of the tile
+                    const int lane_here = here(lane), c = lane_here & 15, q = lane_here >> 4;
 #pragma unroll 1
                     for (int j = 0; j < 32; ++j)
 #pragma unroll
                         for (int db = 0; db < SIZE / 16; ++db) {
                             u32x2 v;
-                            __builtin_memcpy(&v, vt + lds_at<SIZE>(j, 2 * db + (g4 >> 1)) + (g4 & 1) * 8, 8);
+                            __builtin_memcpy(&v, vt + lds_at<SIZE>(j, 2 * db + (q >> 1)) + (q & 1) * 8, 8);
                             const int32_t key = base + 32 * i + j;
 #pragma unroll
                             for (int mb = 0; mb < MB; ++mb) {
@@ -392,34 +385,47 @@ __global__ __launch_bounds__(64 * kFewWaves, SIZE * MB <= 128 ? 2 : 1) void page
                                 }
                             }
                         }
+                    wavefront_fence();
+#pragma unroll 1
+                    for (int j = 0; j < SIZE / 16; ++j) {                  // (each lane has SIZE / 16 of the tile's 16-byte pieces)
+                        const uint32_t at = lds_at<SIZE>(16 * (j & 1) + c, (j >> 1) * 4 + q);
+                        lds_write16(vt, at, without_not_finite<BF16>(lds_read16(vt, at)));
+                    }
+                    wavefront_fence();
+                }
+                const uint32_t row = 4 * g4 + (c16 >> 2), half = (c16 & 1) * 8;
+#pragma unroll
+                for (int db = 0; db < SIZE / 16; ++db) {
+                    const uint32_t chunk = 2 * db + ((c16 >> 1) & 1);
+                    const u32x2 a = lds_read_transposed(vt, lds_at<SIZE>(row, chunk) + half), c = lds_read_transposed(vt, lds_at<SIZE>(row + 16, chunk) + half);
+#pragma unroll
+                    for (int mb = 0; mb < MB; ++mb) acc[mb][db] = mfma16<BF16>(u32x4{a[0], a[1], c[0], c[1]}, pk[mb][i], acc[mb][db]);
                 }
             }
-            if (more) {
 #pragma unroll
-                for (int u = 0; u < NG; ++u) named[u] = named_next[u];
-            }
+            for (int u = 0; u < NG; ++u) named[u] = named_next[u];
         }
 
         // ---- the wavefronts' results to a common maximum: through LDS, row by row
         float *ex = reinterpret_cast<float *>(vt);
+        const int tid = here(threadIdx.x), lane16 = tid & 15, lane4 = (tid >> 4) & 3;
         wavefront_fence();
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
-            l[mb] += __shfl_xor(l[mb], 16, 64);
-            l[mb] += __shfl_xor(l[mb], 32, 64);
-            if (lane < 16) {
-                red_m[wave][16 * mb + lane] = m[mb];
-                red_l[wave][16 * mb + lane] = l[mb];
+            l[mb] = sum_across<true>(l[mb]);
+            if (lane4 == 0) {
+                red_m[wave][16 * mb + lane16] = m[mb];
+                red_l[wave][16 * mb + lane16] = l[mb];
             }
 #pragma unroll
             for (int db = 0; db < SIZE / 16; ++db) {
                 float4v v = acc[mb][db];
                 if constexpr (NORM) v = v * unit[mb];
-                *reinterpret_cast<float4v *>(ex + (16 * mb + c16) * SIZE + 16 * db + 4 * g4) = v;
+                *reinterpret_cast<float4v *>(ex + (16 * mb + lane16) * SIZE + 16 * db + 4 * lane4) = v;
             }
         }
         __syncthreads();
-        for (int e = threadIdx.x; e < 16 * MB * (SIZE / 4); e += 64 * kFewWaves) {
+        for (int e = tid; e < 16 * MB * (SIZE / 4); e += 64 * kFewWaves) {
             const int row = e / (SIZE / 4), d = 4 * (e % (SIZE / 4));
             const uint32_t r = r0 + row;
             if (r >= (uint32_t)rows_all || d >= g.D) continue;

@@ -17,19 +17,24 @@ static nt_status launch_paged_inst(Kernel kern, DeviceOnce &configured, const ch
     return check_launch(name);
 }
 
+template <int SIZE, bool BF16, int KIND, int MB>
+static nt_status launch_paged_few(const PagedArgs &a, int64_t programs, hipStream_t s)
+{
+    static DeviceOnce c[3];
+    const char *name = "paged_few_kernel";
+    if (a.uniform && a.D == SIZE) return launch_paged_inst(paged_few_kernel<BF16, KIND, SIZE, MB, true, true>, c[0], name, few_lds(SIZE, MB), a, programs, s);
+    if (a.uniform) return launch_paged_inst(paged_few_kernel<BF16, KIND, SIZE, MB, true, false>, c[1], name, few_lds(SIZE, MB), a, programs, s);
+    return launch_paged_inst(paged_few_kernel<BF16, KIND, SIZE, MB, false, false>, c[2], name, few_lds(SIZE, MB), a, programs, s);
+}
+
 template <int SIZE, bool BF16, int KIND>
 static nt_status launch_paged_kind(const PagedArgs &a, int rows, int64_t programs, hipStream_t s)
 {
     static_assert(kFewWaves == 4 && kManyWaves == 4, "256 threads");
-    static DeviceOnce few1, few2, few1u, few2u, many;
-    if (rows == 16) {
-        if (a.uniform) return launch_paged_inst(paged_few_kernel<BF16, KIND, SIZE, 1, true>, few1u, "paged_few_kernel", few_lds(SIZE, 1), a, programs, s);
-        return launch_paged_inst(paged_few_kernel<BF16, KIND, SIZE, 1, false>, few1, "paged_few_kernel", few_lds(SIZE, 1), a, programs, s);
-    }
-    if (rows == 32) {
-        if (a.uniform) return launch_paged_inst(paged_few_kernel<BF16, KIND, SIZE, 2, true>, few2u, "paged_few_kernel", few_lds(SIZE, 2), a, programs, s);
-        return launch_paged_inst(paged_few_kernel<BF16, KIND, SIZE, 2, false>, few2, "paged_few_kernel", few_lds(SIZE, 2), a, programs, s);
-    }
+    static DeviceOnce many;
+    if (rows == 16) return launch_paged_few<SIZE, BF16, KIND, 1>(a, programs, s);
+    if constexpr (SIZE < 256)                                              // (two sets of 16 rows of 256 elements do not fit the registers)
+        if (rows == 32) return launch_paged_few<SIZE, BF16, KIND, 2>(a, programs, s);
     return launch_paged_inst(paged_many_kernel<BF16, KIND, SIZE>, many, "paged_many_kernel", many_lds(SIZE), a, programs, s);
 }
 

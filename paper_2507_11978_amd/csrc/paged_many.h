@@ -129,7 +129,7 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
             }
             k = named[u] ? k : u32x4{kNanPair, kNanPair, kNanPair, kNanPair};
             v = named[u] && inside[u] ? v : u32x4{0, 0, 0, 0};
-            if (hidden) odd = odd || any_not_finite<BF16>(v);
+            if (hidden) odd = odd | any_not_finite<BF16>(v);
             const uint32_t at = lds_at<SIZE>(row0 + u * RSTEP, ch);
             lds_write16(smem, copy * BLK + at, k);
             lds_write16(smem, (2 + copy) * BLK + at, v);
@@ -152,9 +152,10 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
     const int gq = lane >> 4, li = lane & 15;
     const uint32_t v_key = 4 * (gq >> 1) + (li >> 2), v_chunk = 2 * (gq & 1) + ((li >> 1) & 1), v_half = (li & 1) * 8;
 
-    auto compute = [&](const int kb, const uint32_t copy) __attribute__((always_inline)) {
+    u32x4 pk[JB][2];                                                       // a block's weights, packed (8-bit caches: times the values' scales)
+    auto weigh = [&](const int kb, const uint32_t copy) __attribute__((always_inline)) {
         const int base = kb * KB;
-        const char *ks_lds = smem + copy * BLK, *vs_lds = smem + (2 + copy) * BLK;
+        const char *ks_lds = smem + copy * BLK;
         // ---- S^T: st[jb][v] <-> key 32 jb + 8 (v / 4) + 4 hi + v % 4, query l32
         float16v st[JB];
 #pragma unroll
@@ -185,7 +186,6 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
                     if (key < row_lo || key >= row_hi) st[jb][v] = out;
                 }
         }
-        const bool careful = hidden && flags[kb % 3] != 0;
         if constexpr (NORM) {
             const float *vs = &scales[copy * 2 * KB + KB];
             float top = 0.f;                                               // the largest scale that the row sees
@@ -213,8 +213,7 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
                     for (int v = 0; v < 16; ++v) ot[db][v] *= shrink;
             }
         }
-        // ---- weights, packed (8-bit caches: times the values' scales), and their sum
-        u32x4 pk[JB][2];
+        // ---- weights and their sum
         float rs;
         auto exponentials = [&](const float m) {
             float sum = 0.f;
@@ -291,39 +290,40 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
             pending = __any(m_new == -INFINITY);
         }
         l_run += rs;
-        // ---- O^T += V^T P^T: k step (jb, s2) lists its 16 keys as 32 jb + 16 s2 + 8 part + 4 hi + 0 .. 3
+    };
+    // ---- O^T += V^T P^T: k step (jb, s2) lists its 16 keys as 32 jb + 16 s2 + 8 part + 4 hi + 0 .. 3
+    auto add_values = [&](const uint32_t copy) __attribute__((always_inline)) {
+        const char *vs_lds = smem + (2 + copy) * BLK;
 #pragma unroll
         for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
             for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
                 for (int db = 0; db < SIZE / 32; ++db) {
-                    u32x2 a = lds_read_transposed(vs_lds, lds_at<SIZE>(32 * jb + 16 * s2 + v_key, 4 * db + v_chunk) + v_half);
-                    u32x2 c = lds_read_transposed(vs_lds, lds_at<SIZE>(32 * jb + 16 * s2 + 8 + v_key, 4 * db + v_chunk) + v_half);
-                    if (careful) {
-                        a = u32x2{without_not_finite<BF16>(a[0]), without_not_finite<BF16>(a[1])};
-                        c = u32x2{without_not_finite<BF16>(c[0]), without_not_finite<BF16>(c[1])};
-                    }
+                    const u32x2 a = lds_read_transposed(vs_lds, lds_at<SIZE>(32 * jb + 16 * s2 + v_key, 4 * db + v_chunk) + v_half);
+                    const u32x2 c = lds_read_transposed(vs_lds, lds_at<SIZE>(32 * jb + 16 * s2 + 8 + v_key, 4 * db + v_chunk) + v_half);
                     ot[db] = mfma32<BF16>(u32x4{a[0], a[1], c[0], c[1]}, pk[jb][s2], ot[db]);
                 }
-        if (careful) {
-            // infinities and NaN of keys that only some rows see: added to those rows alone
+    };
+    // Infinities and NaN of keys that only some rows see: added to those rows alone (a weight of 0 does not silence them)
+    auto add_not_finite = [&](const int kb, const uint32_t copy) {
+        const char *vs_lds = smem + (2 + copy) * BLK;
+        const int half = here(hi);
 #pragma unroll 1
-            for (int key = 0; key < KB; ++key) {
-                const bool sees = base + key >= row_lo && base + key < row_hi;
+        for (int j = 0; j < KB; ++j) {
+            const bool sees = kb * KB + j >= row_lo && kb * KB + j < row_hi;
 #pragma unroll
-                for (int db = 0; db < SIZE / 32; ++db)
+            for (int db = 0; db < SIZE / 32; ++db)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        u32x2 v;
-                        __builtin_memcpy(&v, vs_lds + lds_at<SIZE>(key, 4 * db + q) + hi * 8, 8);
+                for (int q = 0; q < 4; ++q) {
+                    u32x2 v;
+                    __builtin_memcpy(&v, vs_lds + lds_at<SIZE>(j, 4 * db + q) + half * 8, 8);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float x = only_not_finite(widen_one<BF16>(v[e >> 1], e & 1));
-                            ot[db][4 * q + e] += sees ? x : 0.f;
-                        }
+                    for (int e = 0; e < 4; ++e) {
+                        const float x = only_not_finite(widen_one<BF16>(v[e >> 1], e & 1));
+                        ot[db][4 * q + e] += sees ? x : 0.f;
                     }
-            }
+                }
         }
     };
 
@@ -344,7 +344,18 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
             fetch(kb + 1);
             find(kb + 2);
         }
-        if (busy && kb * KB < wave_hi && kb * KB + KB > wave_lo) compute(kb, copy);
+        const bool act = busy && kb * KB < wave_hi && kb * KB + KB > wave_lo;
+        if (act) weigh(kb, copy);
+        if ((kb * KB < seen_lo || kb * KB + KB > seen_hi) && flags[kb % 3] != 0) {         // (workgroup-uniform; rare)
+            if (act) add_not_finite(kb, copy);
+            __syncthreads();
+            for (int u = 0; u < PER; ++u) {                                // ... and taken out of the block
+                const uint32_t at = (2 + copy) * BLK + lds_at<SIZE>(here(row0) + u * RSTEP, ch);
+                lds_write16(smem, at, without_not_finite<BF16>(lds_read16(smem, at)));
+            }
+            __syncthreads();
+        }
+        if (act) add_values(copy);
         if (tid == 0) flags[(kb + 2) % 3] = 0;                             // (read in the pass before this one, set in the next)
         if (more) stash(kb + 1, copy ^ 1);
         __syncthreads();

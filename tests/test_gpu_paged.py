@@ -213,10 +213,10 @@ KINDS = [("f16", "same"), ("bf16", "same"), ("f16", "e4m3"), ("bf16", "e4m3"), (
 
 @pytest.mark.parametrize("dt,kind", KINDS)
 @pytest.mark.parametrize("q_heads,heads,size,page,layout", [(1, 1, 64, 16, "dense"), (8, 2, 128, 16, "heads first"), (6, 6, 80, 24, "dense"), (5, 1, 256, 7, "heads first"),
-                                                            (4, 2, 8, 1, "dense"), (20, 1, 136, 32, "dense")])
+                                                            (4, 2, 8, 1, "dense"), (20, 1, 136, 32, "dense"), (20, 1, 120, 16, "heads first")])
 def test_single_tokens(dt, kind, q_heads, heads, size, page, layout):
     """Lengths around a tile's, a page's and a share's end."""
-    rows = 16 if q_heads // heads <= 16 else 32
+    rows = 16 if q_heads // heads <= 16 else 32 if size <= 128 else 128
     attend([(1, n) for n in (1, 2, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 129, 300)], q_heads, heads, size, page, dt, kind, layout, hints=(1, 0), plan=(rows, False))
 
 
@@ -231,7 +231,8 @@ def test_shared_keys(dt, kind):
     """Long pasts and few programs: shares, their ends inside and beyond the shorter sequences."""
     attend([(1, 4000), (1, 5), (1, 1800), (1, 0)], 8, 2, 128, 16, dt, kind, hints=(1, 4000), plan=(16, True))
     attend([(9, 3000), (40, 41), (1, 2900)], 4, 2, 64, 16, dt, kind, hints=(40, 3000), plan=(128, True))
-    attend([(3, 2500), (2, 900)], 8, 1, 256, 16, dt, kind, hints=(3, 2500), plan=(32, True))
+    attend([(3, 2500), (2, 900)], 8, 1, 128, 16, dt, kind, hints=(3, 2500), plan=(32, True))
+    attend([(3, 2500), (2, 900)], 8, 1, 256, 16, dt, kind, hints=(3, 2500), plan=(128, True))
 
 
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
@@ -343,6 +344,33 @@ def test_values_of_any_size(kind, size_of_v):
         for j in range(0, seqs[0][1], 50):
             b.c[3][int(b.table[0, j // 16]), j % 16] *= 2.0 ** -20
         b.check(b.run(max_queries=hints[0]), f"{size_of_v}, mixed")
+
+
+def test_a_table_without_entries():
+    b = Batch([(1, 0), (2, 0)], 4, 2, 64, 16, "f16")
+    b.table = np.zeros((2, 0), np.int64)
+    for hints in (0, 2):
+        assert (b.run(max_queries=hints) == 0).all()
+    b.lengths = [1, 0]
+    for hints in (0, 2):
+        got = b.run(max_queries=hints)
+        assert torch.isnan(got[0]).all() and (got[1:] == 0).all()
+
+
+@pytest.mark.parametrize("dt,kind", [("f16", "i8"), ("f16", "e4m3"), ("bf16", "e4m3")])
+def test_scales_of_later_tokens(dt, kind):
+    """The scale of a key or value that a token does not see has no part in its result, however large or small or not a number."""
+    for seqs, hints, at in (([(4, 40), (2, 7)], (4, 0), 38), ([(100, 130), (1, 5)], (0, 0), 90)):
+        b = Batch(seqs, 4, 2, 64, 16, dt, kind, seed=9)
+        want = b.run(max_queries=hints[0]).clone()
+        first = at - (seqs[0][1] - seqs[0][0])
+        for scales in (b.c[2], b.c[3]):
+            for value in (2.0 ** 30, 2.0 ** -30, float("nan"), float("inf")):
+                was = scales[int(b.table[0, at // 16]), at % 16].clone()
+                scales[int(b.table[0, at // 16]), at % 16] = value
+                got = b.run(max_queries=hints[0])
+                assert torch.equal(got[:first], want[:first]) and torch.equal(got[seqs[0][0]:], want[seqs[0][0]:])
+                scales[int(b.table[0, at // 16]), at % 16] = was
 
 
 def test_strided_queries_and_outputs():
