@@ -173,10 +173,20 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     if (max_length) length = std::min(length, max_length);
     if (window) length = std::min(length, window + most);
     const int64_t block = rows == kManyRows ? many_keys(built) : few_trip(kind, built);
-    const int64_t wanted = rows == kManyRows ? (base >= 256 ? 1 : 512 / base) : (1024 + base - 1) / base;
-    int64_t splits = std::max<int64_t>(1, std::min(wanted, length / (rows == kManyRows ? 512 : 256)));
-    splits = std::min<int64_t>(splits, kMaxWorkgroups / base);
-    if (getenv("XS") && rows != kManyRows) splits = std::max<int64_t>(1, length / atoi(getenv("XS")));
+    int64_t splits;
+    if (rows == kManyRows) {
+        splits = std::min(base >= 256 ? 1 : 512 / base, length / 512);
+    } else {
+        // As many programs as units, of 48 KB of K and V and more each (us, graph replays: 1 x 8 heads x 128 bf16, 500 keys 12.0 unshared, 9.5 in 6 shares, 2000 32.3 / 10.7
+        // in 21, 32000 434 / 31.0 in 32, 31.2 in 63; 48 heads x 64 f16, 900 12.2 / 10.6 in 4, 12.3 in 3, 8000 60.0 / 24.5 in 4, 28.3 in 8; 300 9.1 / 9.7 in 3).
+        const int64_t key_bytes = 2 * D * es, total = length * key_bytes;
+        // Below 384 KB to a sequence's head not at all: the second launch and the workspace's event are 4 us of the host's time (48 x 900, called: 12.5 us, 13.2).
+        splits = total < (384 << 10) ? 1 : std::min(256 / base, total / (48 << 10));
+        // Where that leaves long programs, 256 KB each: sequences of different lengths fill the units more evenly (64 x 8 heads x 128 bf16, 17 to 4096 keys 154 us
+        // unshared, 134 so, 143 with 512 KB; 2 x 8 heads x 131072 e4m3 135 with 1 MB, 130).
+        if (total / std::max<int64_t>(1, splits) > (5 << 20) / 4) splits = total / (256 << 10);
+    }
+    splits = std::min(std::max<int64_t>(1, splits), kMaxWorkgroups / base);
     int64_t share = ((length + splits - 1) / splits + block - 1) / block * block;
     splits = share ? std::max<int64_t>(1, (length + share - 1) / share) : 1;
     WorkspaceLease lease;

@@ -1,7 +1,7 @@
 // Attention over a paged cache for few query rows per key head: a decoding step, or a few tokens of each sequence.
 //
 // One program per (sequence, key head, share of the keys) has the rows (token, query head of the group) of that sequence, 16 or 32 at a time, so that
-// K and V are read once for all query heads that share them.  Its four wavefronts take the keys in turn, tiles of 32, each with a running maximum m (base-2
+// K and V are read once for all query heads that share them.  Its wavefronts take the keys in turn, tiles of 32, each with a running maximum m (base-2
 // units), sum l and accumulator of its own:
 //   S^T = K Q^T;  p = 2^(c S - m);  l += sum p;  O^T += V^T P^T,
 // brought to a common maximum at the end.  16 x 16 x 32 matrix instructions with the query on the lane axis (lane % 16): the four scores that a lane holds
@@ -15,15 +15,15 @@
 
 namespace nt {
 
-constexpr int kFewWaves = 4;
+constexpr int kFewWaves = 4;                                             // (8 measured no gain: 48 heads x 900 f16 12.2 us with four, 13.1)
 constexpr size_t few_lds(int size, int mb) { return (size_t)kFewWaves * mb * 64 * size; }        // V's 32 keys (64 * size bytes), later 16 * mb rows of fp32 outputs
 // 32-key tiles of a trip, which a wavefront has in flight: two, or one where a tile of K and V is 16 KB
 constexpr int few_tiles(int kind, int size) { return size * (kind == CACHE_SAME ? 2 : 1) >= 256 ? 1 : 2; }
 constexpr int few_trip(int kind, int size) { return 32 * few_tiles(kind, size); }        // keys
 
-// Wavefronts per SIMD that the registers are shared out for.  Three where they suffice: a program's start -- the sequence's bounds, its pages, the first
-// keys, each awaited in turn -- is hidden by the other programs of its unit
-constexpr int few_resident(int kind, int size, int mb) { return mb == 1 && (size == 64 || (size == 128 && kind == CACHE_SAME)) ? 3 : size * mb <= 128 ? 2 : 1; }
+// Wavefronts per SIMD that the registers are shared out for: three at head size 64, whose trips are half as long (32 x 48 heads x 2047 int8 72 us with two, 63).
+// At 128 three do not help (64 x 8 heads x 4096 bf16 134 us with two, 144): 128 KB in flight per unit are enough, and more only wait for each other.
+constexpr int few_resident(int size, int mb) { return mb == 1 && size == 64 ? 3 : size * mb <= 128 ? 2 : 1; }
 
 // a * s, 32 by 64 bits
 __device__ __forceinline__ int64_t times(uint32_t a, int64_t s)
@@ -34,7 +34,7 @@ __device__ __forceinline__ int64_t times(uint32_t a, int64_t s)
 // UNIFORM: page_size is a multiple of 16, so that 16 keys that begin at a multiple of 16 lie on one page: the table is read and the addresses are made
 // once for a wavefront, on the scalar unit, and a lane's part is an offset that never changes.
 template <bool BF16, int KIND, int SIZE, int MB, bool UNIFORM, bool FULL>
-__global__ __launch_bounds__(64 * kFewWaves, few_resident(KIND, SIZE, MB)) void paged_few_kernel(const PagedArgs g)
+__global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_few_kernel(const PagedArgs g)
 {
     constexpr int KS = SIZE / 32;                                          // k steps of the first product
     constexpr int NV = KIND == CACHE_SAME ? SIZE / 32 : SIZE / 64;         // 16-byte loads per lane, 16 keys and tensor
@@ -47,10 +47,20 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(KIND, SIZE, MB)) void 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c16 = lane & 15, g4 = lane >> 4;
     char *vt = smem + wave * (64 * SIZE * MB);
 
-    int w = blockIdx.x;
-    const int h = w % g.Hkv;                                               // (consecutive programs, on different XCDs, have different heads)
-    w /= g.Hkv;
-    const int split = w % g.splits, b = w / g.splits;
+    // Consecutive programs go to different XCDs (number mod 8).  The heads of one share lie side by side in memory: one XCD has them, one after the other, and
+    // the pages of an eighth of the shares, not an eighth of all pages' bytes
+    const uint32_t w = blockIdx.x, heads = g.Hkv, items = (uint32_t)g.B * g.splits, whole = (items & ~7u) * heads;
+    uint32_t item, h;
+    if (w < whole) {
+        const uint32_t j = w >> 3;
+        const uint32_t group = j / heads;
+        item = group * 8 + ((w + group) & 7);
+        h = j % heads;
+    } else {
+        item = w / heads;
+        h = w % heads;
+    }
+    const int split = item % g.splits, b = item / g.splits;
     typedef const __attribute__((address_space(4))) int32_t *ScalarTable;
     const int32_t *pages = g.table + (int64_t)b * g.t_sb;
     const char *Kh = g.K + (int64_t)h * g.k_sh * ES, *Vh = g.V + (int64_t)h * g.v_sh * ES;
@@ -165,6 +175,12 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(KIND, SIZE, MB)) void 
             find(t + kFewWaves);
         }
 
+        // Q is waited for here: at its first use inside the loop the wait would be one for everything in flight, in every trip
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[mb][ks]));
+
         float m[MB], l[MB];
         float4v acc[MB][SIZE / 16];
 #pragma unroll
@@ -182,8 +198,6 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(KIND, SIZE, MB)) void 
 
         for (; t < t_end; t += kFewWaves) {
             const int base = t * TRIP, next = t + kFewWaves;
-            // (head size 128: LDS addresses are worked out anew in each trip, 30 instructions that cost less than their registers)
-            const int lane = SIZE == 128 ? here(threadIdx.x & 63) : (int)threadIdx.x & 63, c16 = lane & 15, g4 = lane >> 4;
             const bool more = next < t_end;
             // ---- S^T: lane (c16, g4) gets query c16, keys 16 u + 4 g4 + 0 .. 3
             float4v st[MB][NG];
@@ -393,13 +407,29 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(KIND, SIZE, MB)) void 
                     }
                     wavefront_fence();
                 }
+                // (four blocks' reads are on their way while the four before them are multiplied)
                 const uint32_t row = 4 * g4 + (c16 >> 2), half = (c16 & 1) * 8;
+                u32x2 frag[2][4][2];
+                auto read_four = [&](int q) {
 #pragma unroll
-                for (int db = 0; db < SIZE / 16; ++db) {
-                    const uint32_t chunk = 2 * db + ((c16 >> 1) & 1);
-                    const u32x2 a = lds_read_transposed(vt, lds_at<SIZE>(row, chunk) + half), c = lds_read_transposed(vt, lds_at<SIZE>(row + 16, chunk) + half);
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t chunk = 2 * (4 * q + j) + ((c16 >> 1) & 1);
+                        frag[q & 1][j][0] = lds_read_transposed(vt, lds_at<SIZE>(row, chunk) + half);
+                        frag[q & 1][j][1] = lds_read_transposed(vt, lds_at<SIZE>(row + 16, chunk) + half);
+                    }
+                };
+                read_four(0);
 #pragma unroll
-                    for (int mb = 0; mb < MB; ++mb) acc[mb][db] = mfma16<BF16>(u32x4{a[0], a[1], c[0], c[1]}, pk[mb][i], acc[mb][db]);
+                for (int q = 0; q < SIZE / 64; ++q) {
+                    if (q + 1 < SIZE / 64) read_four(q + 1);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const u32x2 a = frag[q & 1][j][0], c = frag[q & 1][j][1];
+#pragma unroll
+                        for (int mb = 0; mb < MB; ++mb) acc[mb][4 * q + j] = mfma16<BF16>(u32x4{a[0], a[1], c[0], c[1]}, pk[mb][i], acc[mb][4 * q + j]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
 #pragma unroll
