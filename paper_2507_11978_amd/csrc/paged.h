@@ -156,6 +156,12 @@ __device__ __forceinline__ float unit_above(float top)
     return __builtin_bit_cast(float, up < 0x03800000u ? 0x03800000u : up > 0x7e000000u ? 0x7e000000u : up);
 }
 
+// a * s, 32 by 64 bits
+__device__ __forceinline__ int64_t times(uint32_t a, int64_t s)
+{
+    return (int64_t)((uint64_t)a * (uint32_t)s + ((uint64_t)(a * (uint32_t)((uint64_t)s >> 32)) << 32));
+}
+
 // ---- the attention kernels' arguments (strides in elements)
 struct PagedArgs {
     const uint16_t *Q;
@@ -173,6 +179,7 @@ struct PagedArgs {
     int32_t tiles;                     // of query rows, all sequences together (paged_many)
     int32_t causal, window;            // window 0: none
     int32_t uniform;                   // 16 keys from a multiple of 16 on lie on one page, at offsets of 32 bits from the first
+    int32_t aligned;                   // every row of the cache begins at a multiple of 16 bytes
     int32_t splits, split_keys;        // the keys of a tile are shared out over `splits` programs, split_keys each (the last: what is left)
     Divider page, group;               // by page_size, by G
     float scale_log2e;                 // scale * log2(e): exponentials are taken in base 2

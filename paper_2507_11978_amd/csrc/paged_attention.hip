@@ -157,6 +157,7 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     a.window = (int32_t)std::min<int64_t>(window, 1 << 30);
     const int64_t es = kind == CACHE_SAME ? 2 : 1, most_bytes = (1LL << 31) - 4096;
     a.uniform = page_size % 16 == 0 && a.k_ss >= 0 && a.k_ss < most_bytes / (16 * es) && a.v_ss >= 0 && a.v_ss < most_bytes / (16 * es);
+    a.aligned = (((uintptr_t)a.K | (uintptr_t)a.V | (uint64_t)((a.k_sp | a.k_ss | a.k_sh | a.v_sp | a.v_ss | a.v_sh) * es)) & 15) == 0;
     a.page = divider_of((uint32_t)page_size);
     a.group = divider_of((uint32_t)a.G);
     a.scale_log2e = (scale == 0.f ? 1.0f / sqrtf((float)D) : scale) * 1.4426950408889634f;

@@ -25,12 +25,6 @@ constexpr int few_trip(int kind, int size) { return 32 * few_tiles(kind, size); 
 // At 128 three do not help (64 x 8 heads x 4096 bf16 134 us with two, 144): 128 KB in flight per unit are enough, and more only wait for each other.
 constexpr int few_resident(int size, int mb) { return mb == 1 && size == 64 ? 3 : size * mb <= 128 ? 2 : 1; }
 
-// a * s, 32 by 64 bits
-__device__ __forceinline__ int64_t times(uint32_t a, int64_t s)
-{
-    return (int64_t)((uint64_t)a * (uint32_t)s + ((uint64_t)(a * (uint32_t)((uint64_t)s >> 32)) << 32));
-}
-
 // UNIFORM: page_size is a multiple of 16, so that 16 keys that begin at a multiple of 16 lie on one page: the table is read and the addresses are made
 // once for a wavefront, on the scalar unit, and a lane's part is an offset that never changes.
 template <bool BF16, int KIND, int SIZE, int MB, bool UNIFORM, bool FULL>

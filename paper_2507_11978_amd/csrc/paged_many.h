@@ -7,8 +7,9 @@
 // sees are not computed.  With an 8-bit cache the codes are widened on their way to LDS, a key's scale multiplies its scores in fp32 and a value's scale
 // its weight, so that nothing is rounded but the weights, as in a 16-bit cache.
 //
-// K and V travel through registers, one block ahead of the arithmetic, into one of two LDS copies each.  What bounds it is the matrix pipe: per block and
-// wavefront 32 instructions of 32 cycles (128 elements) beside some 90 vector instructions.
+// FAST (whole rows at addresses that are multiples of 16 bytes, pages of a multiple of 16 keys): the rows that a wavefront moves with one load lie on one page; the table is read and the addresses are
+// made on the scalar unit.  A 16-bit cache then travels straight into LDS, one block ahead, codes through registers, 16 at a time.  Other caches: 8
+// elements to a lane through registers, every lane with an address of its own.
 #pragma once
 #include "paged.h"
 
@@ -20,10 +21,12 @@ constexpr size_t many_block(int size) { return (size_t)many_keys(size) * size * 
 // [K0][K1][V0][V1], scales of two blocks (K's, then V's), three flags
 constexpr size_t many_lds(int size) { return 4 * many_block(size) + 2 * 2 * many_keys(size) * 4 + 16; }
 
-template <bool BF16, int KIND, int SIZE>
+template <bool BF16, int KIND, int SIZE, bool FAST>
 __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 : 1) void paged_many_kernel(const PagedArgs g)
 {
-    constexpr int KB = many_keys(SIZE), JB = KB / 32, CH = SIZE / 8, PER = KB * CH / 256, RSTEP = 256 / CH;
+    constexpr bool DMA = FAST && KIND == CACHE_SAME;
+    constexpr int EPL = FAST && KIND != CACHE_SAME ? 16 : 8;               // elements that a lane moves at a time
+    constexpr int KB = many_keys(SIZE), JB = KB / 32, CH = SIZE / EPL, PER = KB * CH / 256, RSTEP = 256 / CH;
     constexpr int ES = KIND == CACHE_SAME ? 2 : 1;
     constexpr uint32_t BLK = many_block(SIZE);
     constexpr bool NORM = KIND != CACHE_SAME && !BF16;
@@ -80,63 +83,110 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
         }
     }
 
-    // ---- a block on its way: thread tid moves chunk tid % CH of rows tid / CH + u * RSTEP
+    // ---- a block on its way: thread tid moves piece tid % CH of rows tid / CH + u * RSTEP, a wavefront RSTEP / 4 rows from row wave * RSTEP / 4 on
     const int ch = tid % CH, row0 = tid / CH;
-    typedef typename std::conditional<KIND == CACHE_SAME, u32x4, u32x2>::type Piece;
-    Piece kr[PER], vr[PER];
+    typedef typename std::conditional<EPL * ES == 16, u32x4, u32x2>::type Piece;
+    Piece kr[DMA ? 1 : PER], vr[DMA ? 1 : PER];
     float sc = 0.f;
-    int32_t id[PER], sid = -1;                                             // pages of the block that is fetched next; sid: of the thread's scale
-    bool named[PER], inside[PER];
+    int32_t id[PER], sid = -1;                                             // the table's entries for the block that is fetched next; sid: for the thread's scale
+    uint32_t named = 0;                                                    // bit u: a page is named for the thread's row u (of the block that was fetched last)
+    typedef const __attribute__((address_space(4))) int32_t *ScalarTable;
+    auto entry = [&](uint32_t index) { return index < (uint32_t)g.width ? index : g.width > 0 ? g.width - 1 : 0; };      // (see paged_few.h)
+    auto row_of = [&](int kb, int u) { return (uint32_t)(kb * KB + u * RSTEP + (FAST ? wave * (RSTEP / 4) : row0)); };
     auto find = [&](int kb) {
 #pragma unroll
-        for (int u = 0; u < PER; ++u) id[u] = page_at(pages, divide((uint32_t)(kb * KB + row0 + u * RSTEP), g.page), g.width, g.pages);
-        if constexpr (KIND != CACHE_SAME) sid = page_at(pages, divide((uint32_t)(kb * KB + tid % KB), g.page), g.width, g.pages);
+        for (int u = 0; u < PER; ++u) {
+            const uint32_t index = entry(divide(row_of(kb, u), g.page));
+            id[u] = FAST ? ((ScalarTable)pages)[index] : pages[index];
+        }
+        if constexpr (KIND != CACHE_SAME) sid = pages[entry(divide((uint32_t)(kb * KB + tid % KB), g.page))];
     };
-    auto fetch = [&](int kb) {
+    // byte offsets within the wavefront's rows (FAST).  Straight into LDS: a lane's 16 bytes land at lane * 16, so it fetches the piece that belongs there; of
+    // rows that lie 8 apart (head size 256) the order of the pieces differs in its last bit.
+    const int lane_row = FAST ? lane / CH : 0;
+    const uint32_t at_piece = DMA ? (uint32_t)(lane % CH) ^ chunk_order<SIZE>((uint32_t)(wave * (RSTEP / 4) + lane_row)) : (uint32_t)(lane % CH);
+    const uint32_t kl = FAST ? (uint32_t)(lane_row * (int32_t)g.k_ss * ES) + 16 * at_piece : 0, vl = FAST ? (uint32_t)(lane_row * (int32_t)g.v_ss * ES) + 16 * at_piece : 0;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
+    auto fetch = [&](int kb, uint32_t copy) {
+        named = 0;
 #pragma unroll
         for (int u = 0; u < PER; ++u) {
-            const int32_t key = kb * KB + row0 + u * RSTEP;
-            named[u] = id[u] >= 0;
-            inside[u] = key >= keys.lo && key < keys.hi;
-            const int64_t page = named[u] ? id[u] : 0, at = (uint32_t)key - divide((uint32_t)key, g.page) * g.page.d;
-            kr[u] = vr[u] = Piece{};
-            if (8 * ch < g.D) {
-                __builtin_memcpy(&kr[u], Kh + (page * g.k_sp + at * g.k_ss + 8 * ch) * ES, sizeof(Piece));
-                __builtin_memcpy(&vr[u], Vh + (page * g.v_sp + at * g.v_ss + 8 * ch) * ES, sizeof(Piece));
+            const uint32_t key = row_of(kb, u), index = divide(key, g.page), at = key - index * g.page.d;
+            const bool ok = index < (uint32_t)g.width && (uint32_t)id[u] < (uint32_t)g.pages;
+            const uint32_t page = ok ? id[u] : 0;
+            named |= (ok ? 1u : 0u) << u;
+            const char *kp = Kh + (times(page, g.k_sp) + times(at, g.k_ss)) * ES, *vp = Vh + (times(page, g.v_sp) + times(at, g.v_ss)) * ES;
+            if constexpr (DMA) {
+                const uint32_t flip = RSTEP == 8 && (u & 1) ? (at_piece & 1 ? 0u - 16u : 16u) : 0u, to = lds0 + copy * BLK + (uint32_t)((u * RSTEP + wave * (RSTEP / 4)) * SIZE * 2);
+                dma16(kp, kl + flip, to);
+                dma16(vp, vl + flip, to + 2 * BLK);
+            } else if constexpr (FAST) {
+                __builtin_memcpy(&kr[u], kp + kl, 16);
+                __builtin_memcpy(&vr[u], vp + vl, 16);
+            } else {
+                const int d = 8 * ch <= g.D - 8 ? 8 * ch : g.D - 8;        // (no elements there: the row's last ones, see stash)
+                __builtin_memcpy(&kr[u], kp + d * ES, sizeof(Piece));
+                __builtin_memcpy(&vr[u], vp + d * ES, sizeof(Piece));
             }
         }
         if constexpr (KIND != CACHE_SAME) {
-            if (tid < 2 * KB) {
-                const uint32_t key = kb * KB + tid % KB;
-                const int64_t page = sid >= 0 ? sid : 0, at = key - divide(key, g.page) * g.page.d;
-                sc = tid < KB ? g.KS[page * g.ks_sp + at * g.ks_ss + (int64_t)h * g.ks_sh] : g.VS[page * g.vs_sp + at * g.vs_ss + (int64_t)h * g.vs_sh];
-            }
+            const uint32_t key = kb * KB + tid % KB, index = divide(key, g.page), at = key - index * g.page.d;
+            const uint32_t page = index < (uint32_t)g.width && (uint32_t)sid < (uint32_t)g.pages ? sid : 0;
+            sc = tid < KB ? g.KS[times(page, g.ks_sp) + times(at, g.ks_ss) + (int64_t)h * g.ks_sh] : g.VS[times(page, g.vs_sp) + times(at, g.vs_ss) + (int64_t)h * g.vs_sh];
         }
     };
-    // into LDS copy `copy`.  Keys that no page is named for become NaN, their values, and those of keys outside the range, zeros (see paged_few.h)
+    // The fetched block is where the other wavefronts read it, in LDS copy `copy`, once they have passed a barrier behind this.  Keys that no page is named for
+    // become NaN, their values, and those of keys outside the range, zeros (see paged_few.h)
     auto stash = [&](int kb, uint32_t copy) {
         const bool hidden = kb * KB < seen_lo || kb * KB + KB > seen_hi;   // from some row
-        bool odd = false;
-#pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            u32x4 k, v;
-            if constexpr (KIND == CACHE_SAME) {
-                k = kr[u];
-                v = vr[u];
-            } else {
-                k = widen8<BF16, KIND>(kr[u]);
-                v = widen8<BF16, KIND>(vr[u]);
+        if constexpr (DMA) {
+            NT_WAIT_VMCNT(0);
+            asm volatile("" ::: "memory");
+            if (hidden || kb * KB < keys.lo || kb * KB + KB > keys.hi || named != (1u << PER) - 1) {           // wavefront-uniform
+                bool odd = false;
+#pragma unroll 1
+                for (int u = 0; u < PER; ++u) {
+                    const int32_t r = u * RSTEP + wave * (RSTEP / 4) + here(lane) / CH, key = kb * KB + r;
+                    const uint32_t at = copy * BLK + (uint32_t)((u * RSTEP + wave * (RSTEP / 4)) * SIZE * 2 + here(lane) * 16);
+                    if (!((named >> u) & 1)) lds_write16(smem, at, u32x4{kNanPair, kNanPair, kNanPair, kNanPair});
+                    if (!((named >> u) & 1) || key < keys.lo || key >= keys.hi) lds_write16(smem, at + 2 * BLK, u32x4{0, 0, 0, 0});
+                    else if (hidden) odd = odd | any_not_finite<BF16>(lds_read16(smem, at + 2 * BLK));
+                }
+                if (odd) flags[kb % 3] = 1;
             }
-            k = named[u] ? k : u32x4{kNanPair, kNanPair, kNanPair, kNanPair};
-            v = named[u] && inside[u] ? v : u32x4{0, 0, 0, 0};
-            if (hidden) odd = odd | any_not_finite<BF16>(v);
-            const uint32_t at = lds_at<SIZE>(row0 + u * RSTEP, ch);
-            lds_write16(smem, copy * BLK + at, k);
-            lds_write16(smem, (2 + copy) * BLK + at, v);
+        } else {
+            bool odd = false;
+#pragma unroll
+            for (int u = 0; u < PER; ++u) {
+                const uint32_t r = u * RSTEP + row0;
+                const int32_t key = kb * KB + (int32_t)r;
+                const bool page = (named >> u) & 1, good = page && key >= keys.lo && key < keys.hi;
+#pragma unroll
+                for (int half = 0; half < EPL / 8; ++half) {
+                    u32x4 k, v;
+                    if constexpr (KIND == CACHE_SAME) {
+                        k = kr[u];
+                        v = vr[u];
+                    } else if constexpr (FAST) {
+                        k = widen8<BF16, KIND>(u32x2{kr[u][2 * half], kr[u][2 * half + 1]});
+                        v = widen8<BF16, KIND>(u32x2{vr[u][2 * half], vr[u][2 * half + 1]});
+                    } else {
+                        k = widen8<BF16, KIND>(u32x2{kr[u][0], kr[u][1]});
+                        v = widen8<BF16, KIND>(u32x2{vr[u][0], vr[u][1]});
+                    }
+                    if (!FAST && 8 * ch >= g.D) k = v = u32x4{0, 0, 0, 0};
+                    k = page ? k : u32x4{kNanPair, kNanPair, kNanPair, kNanPair};
+                    v = good ? v : u32x4{0, 0, 0, 0};
+                    if (hidden) odd = odd | any_not_finite<BF16>(v);
+                    const uint32_t at = lds_at<SIZE>(r, EPL / 8 * ch + half);
+                    lds_write16(smem, copy * BLK + at, k);
+                    lds_write16(smem, (2 + copy) * BLK + at, v);
+                }
+            }
+            if constexpr (KIND != CACHE_SAME)
+                if (tid < 2 * KB) scales[copy * 2 * KB + tid] = sc;
+            if (odd) flags[kb % 3] = 1;
         }
-        if constexpr (KIND != CACHE_SAME)
-            if (tid < 2 * KB) scales[copy * 2 * KB + tid] = sc;
-        if (odd) flags[kb % 3] = 1;
     };
 
     float16v ot[SIZE / 32];
@@ -333,15 +383,18 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
     __syncthreads();
     if (kb < k_end) {                                                      // (workgroup-uniform, as the loop's count)
         find(kb);
-        fetch(kb);
+        fetch(kb, 0);
         find(kb + 1);
+        // (Q is waited for here: inside the loop the wait would be one for everything in flight)
+#pragma unroll
+        for (int ks = 0; ks < SIZE / 16; ++ks) asm volatile("" : "+v"(qf[ks]));
         stash(kb, 0);
     }
     __syncthreads();
     for (uint32_t copy = 0; kb < k_end; ++kb, copy ^= 1) {
         const bool more = kb + 1 < k_end;
         if (more) {
-            fetch(kb + 1);
+            fetch(kb + 1, copy ^ 1);
             find(kb + 2);
         }
         const bool act = busy && kb * KB < wave_hi && kb * KB + KB > wave_lo;
@@ -349,8 +402,8 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
         if ((kb * KB < seen_lo || kb * KB + KB > seen_hi) && flags[kb % 3] != 0) {         // (workgroup-uniform; rare)
             if (act) add_not_finite(kb, copy);
             __syncthreads();
-            for (int u = 0; u < PER; ++u) {                                // ... and taken out of the block
-                const uint32_t at = (2 + copy) * BLK + lds_at<SIZE>(here(row0) + u * RSTEP, ch);
+            for (int i = here(tid); i < KB * (SIZE / 8); i += 256) {       // ... and taken out of the block
+                const uint32_t at = (2 + copy) * BLK + 16 * i;
                 lds_write16(smem, at, without_not_finite<BF16>(lds_read16(smem, at)));
             }
             __syncthreads();

@@ -227,6 +227,15 @@ def test_chunks(dt, kind, q_heads, heads, size, page, layout):
 
 
 @pytest.mark.parametrize("dt,kind", KINDS)
+@pytest.mark.parametrize("size", [64, 128, 256])
+@pytest.mark.parametrize("layout", ["padded", "dense"])
+def test_pages_of_whole_groups_of_keys(dt, kind, size, layout):
+    """Whole rows, 32 keys to a page: rows at multiples of 16 bytes, and rows that begin anywhere."""
+    attend([(70, 150), (1, 97), (33, 33), (130, 131)], 2, 2, size, 32, dt, kind, layout, seed=7, plan=(128, None))
+    attend([(1, 150), (2, 97), (1, 1)], 2, 2, size, 32, dt, kind, layout, seed=8, hints=(2, 0), plan=(16, None))
+
+
+@pytest.mark.parametrize("dt,kind", KINDS)
 def test_shared_keys(dt, kind):
     """Long pasts and few programs: shares, their ends inside and beyond the shorter sequences."""
     attend([(1, 4000), (1, 5), (1, 1800), (1, 0)], 8, 2, 128, 16, dt, kind, hints=(1, 4000), plan=(16, True))
