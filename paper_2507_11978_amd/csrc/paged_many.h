@@ -8,7 +8,7 @@
 // its weight, so that nothing is rounded but the weights, as in a 16-bit cache.
 //
 // FAST (whole rows at addresses that are multiples of 16 bytes, pages of a multiple of 16 keys): the rows that a wavefront moves with one load lie on one page; the table is read and the addresses are
-// made on the scalar unit.  A 16-bit cache then travels straight into LDS, one block ahead, codes through registers, 16 at a time.  Other caches: 8
+// made by one lane for all.  A 16-bit cache then travels straight into LDS, one block ahead, codes through registers, 16 at a time.  Other caches: 8
 // elements to a lane through registers, every lane with an address of its own.
 #pragma once
 #include "paged.h"
@@ -90,15 +90,15 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
     float sc = 0.f;
     int32_t id[PER], sid = -1;                                             // the table's entries for the block that is fetched next; sid: for the thread's scale
     uint32_t named = 0;                                                    // bit u: a page is named for the thread's row u (of the block that was fetched last)
-    typedef const __attribute__((address_space(4))) int32_t *ScalarTable;
+    // FAST: lane u has what is the same for all of a wavefront's row u: its table entry and its address in K, lane PER + u that in V
+    const bool of_v = (lane / PER) & 1;
+    const int64_t lane_sp = of_v ? g.v_sp : g.k_sp, lane_ss = of_v ? g.v_ss : g.k_ss;
+    const char *const lane_base = of_v ? Vh : Kh;
     auto entry = [&](uint32_t index) { return index < (uint32_t)g.width ? index : g.width > 0 ? g.width - 1 : 0; };      // (see paged_few.h)
     auto row_of = [&](int kb, int u) { return (uint32_t)(kb * KB + u * RSTEP + (FAST ? wave * (RSTEP / 4) : row0)); };
     auto find = [&](int kb) {
 #pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            const uint32_t index = entry(divide(row_of(kb, u), g.page));
-            id[u] = FAST ? ((ScalarTable)pages)[index] : pages[index];
-        }
+        for (int u = 0; u < (FAST ? 1 : PER); ++u) id[u] = pages[entry(divide(row_of(kb, FAST ? lane % PER : u), g.page))];
         if constexpr (KIND != CACHE_SAME) sid = pages[entry(divide((uint32_t)(kb * KB + tid % KB), g.page))];
     };
     // byte offsets within the wavefront's rows (FAST).  Straight into LDS: a lane's 16 bytes land at lane * 16, so it fetches the piece that belongs there; of
@@ -109,24 +109,38 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
     auto fetch = [&](int kb, uint32_t copy) {
         named = 0;
+        const char *address[FAST ? 1 : PER][2];
 #pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            const uint32_t key = row_of(kb, u), index = divide(key, g.page), at = key - index * g.page.d;
+        for (int u = 0; u < (FAST ? 1 : PER); ++u) {
+            const uint32_t key = row_of(kb, FAST ? lane % PER : u), index = divide(key, g.page), at = key - index * g.page.d;
             const bool ok = index < (uint32_t)g.width && (uint32_t)id[u] < (uint32_t)g.pages;
             const uint32_t page = ok ? id[u] : 0;
-            named |= (ok ? 1u : 0u) << u;
-            const char *kp = Kh + (times(page, g.k_sp) + times(at, g.k_ss)) * ES, *vp = Vh + (times(page, g.v_sp) + times(at, g.v_ss)) * ES;
+            if constexpr (FAST) {
+                named = (uint32_t)__ballot(ok) & ((1u << PER) - 1);
+                address[0][0] = lane_base + (times(page, lane_sp) + times(at, lane_ss)) * ES;
+            } else {
+                named |= (ok ? 1u : 0u) << u;
+                address[u][0] = Kh + (times(page, g.k_sp) + times(at, g.k_ss)) * ES;
+                address[u][1] = Vh + (times(page, g.v_sp) + times(at, g.v_ss)) * ES;
+            }
+        }
+        auto of_lane = [&](int l) {
+            const uint64_t p = reinterpret_cast<uint64_t>(address[0][0]);
+            return reinterpret_cast<const char *>((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)p, l) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(p >> 32), l) << 32);
+        };
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
             if constexpr (DMA) {
                 const uint32_t flip = RSTEP == 8 && (u & 1) ? (at_piece & 1 ? 0u - 16u : 16u) : 0u, to = lds0 + copy * BLK + (uint32_t)((u * RSTEP + wave * (RSTEP / 4)) * SIZE * 2);
-                dma16(kp, kl + flip, to);
-                dma16(vp, vl + flip, to + 2 * BLK);
+                dma16(of_lane(u), kl + flip, to);
+                dma16(of_lane(PER + u), vl + flip, to + 2 * BLK);
             } else if constexpr (FAST) {
-                __builtin_memcpy(&kr[u], kp + kl, 16);
-                __builtin_memcpy(&vr[u], vp + vl, 16);
+                __builtin_memcpy(&kr[u], of_lane(u) + kl, 16);
+                __builtin_memcpy(&vr[u], of_lane(PER + u) + vl, 16);
             } else {
                 const int d = 8 * ch <= g.D - 8 ? 8 * ch : g.D - 8;        // (no elements there: the row's last ones, see stash)
-                __builtin_memcpy(&kr[u], kp + d * ES, sizeof(Piece));
-                __builtin_memcpy(&vr[u], vp + d * ES, sizeof(Piece));
+                __builtin_memcpy(&kr[u], address[u][0] + d * ES, sizeof(Piece));
+                __builtin_memcpy(&vr[u], address[u][1] + d * ES, sizeof(Piece));
             }
         }
         if constexpr (KIND != CACHE_SAME) {
@@ -209,12 +223,13 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
         // ---- S^T: st[jb][v] <-> key 32 jb + 8 (v / 4) + 4 hi + v % 4, query l32
         float16v st[JB];
 #pragma unroll
-        for (int jb = 0; jb < JB; ++jb) {
+        for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
             for (int v = 0; v < 16; ++v) st[jb][v] = 0.f;
 #pragma unroll
-            for (int ks = 0; ks < SIZE / 16; ++ks) st[jb] = mfma32<BF16>(lds_read16(ks_lds, lds_at<SIZE>(32 * jb + l32, 2 * ks + hi)), qf[ks], st[jb]);
-        }
+        for (int ks = 0; ks < SIZE / 16; ++ks)                             // (two chains of products, in turn)
+#pragma unroll
+            for (int jb = 0; jb < JB; ++jb) st[jb] = mfma32<BF16>(lds_read16(ks_lds, lds_at<SIZE>(32 * jb + l32, 2 * ks + hi)), qf[ks], st[jb]);
         if constexpr (KIND != CACHE_SAME) {
 #pragma unroll
             for (int jb = 0; jb < JB; ++jb)
