@@ -162,7 +162,8 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     a.group = divider_of((uint32_t)a.G);
     a.scale_log2e = (scale == 0.f ? 1.0f / sqrtf((float)D) : scale) * 1.4426950408889634f;
 
-    // Up to 32 rows per key head: the kernel whose wavefronts share the keys, else the one whose wavefronts share the rows.
+    // Up to 32 rows per key head: the kernel whose wavefronts share the keys, else the one whose wavefronts share the rows (us, 8 heads x 128 bf16, 32 rows: 1 x 1000
+    // keys 14.0, by the other 27.4, 1 x 8000 18.5 / 25.5, 32 x 2000 57.7 / 81.0; 4 x 16 heads x 64 f16, 8000 35.3 / 42.1).
     const int64_t most = max_queries && max_queries < T ? max_queries : T, group_rows = most * a.G;
     const int built = D <= 64 ? 64 : D <= 128 ? 128 : 256;
     const int rows = group_rows <= 16 ? 16 : group_rows <= 32 && built < 256 ? 32 : kManyRows;
@@ -176,7 +177,9 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     const int64_t block = rows == kManyRows ? many_keys(built) : few_trip(kind, built);
     int64_t splits;
     if (rows == kManyRows) {
-        splits = std::min(base >= 256 ? 1 : 512 / base, length / 512);
+        // Two programs for a unit, of 192 keys each and more (us, graph replays, 32/8 heads x 128 bf16: 64 queries x 600 keys 21.6 unshared, 15.8 in 3 shares,
+        // 1000 29.9 / 17.9 in 4, 20000 526 / 49.5 in 32; 200 x 4000 109 / 38.4 in 8, 60.3 in 16; 7 x 200 in windows of 512 32.0 / 32.9 in 3).
+        splits = std::min(base >= 256 ? 1 : 512 / base, length / 192);
     } else {
         // As many programs as units, of 48 KB of K and V and more each (us, graph replays: 1 x 8 heads x 128 bf16, 500 keys 12.0 unshared, 9.5 in 6 shares, 2000 32.3 / 10.7
         // in 21, 32000 434 / 31.0 in 32, 31.2 in 63; 48 heads x 64 f16, 900 12.2 / 10.6 in 4, 12.3 in 3, 8000 60.0 / 24.5 in 4, 28.3 in 8; 300 9.1 / 9.7 in 3).
