@@ -178,7 +178,8 @@ struct PagedArgs {
     int32_t width, pages;              // entries of a table row, pages of the cache
     int32_t tiles;                     // of query rows, all sequences together (paged_many)
     int32_t causal, window;            // window 0: none
-    int32_t uniform;                   // 16 keys from a multiple of 16 on lie on one page, at offsets of 32 bits from the first
+    int32_t near;                      // offsets within 16 rows of a page are not negative and fit 32 bits
+    int32_t uniform;                   // ... and 16 keys from a multiple of 16 on lie on one page
     int32_t aligned;                   // every row of the cache begins at a multiple of 16 bytes
     int32_t splits, split_keys;        // the keys of a tile are shared out over `splits` programs, split_keys each (the last: what is left)
     Divider page, group;               // by page_size, by G

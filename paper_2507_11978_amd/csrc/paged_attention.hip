@@ -12,7 +12,8 @@ namespace nt {
 
 // WAVES wavefronts per row (token, query head): groups of LANES lanes, 4 elements to a lane, take the shares in turn, eight of them in flight at a time; the
 // groups' sums meet within a wavefront and then in LDS.  One wavefront has many rows to hide behind where the shares are few; four make the
-// chain of 64 shares of a single long sequence short (2 x 32 rows of 128, 64 shares: 28 us with one, two of a group's loads in flight).
+// chain of 64 shares of a single long sequence short (2 x 32 rows of 128, 64 shares: 28 us with one, two of a group's loads in flight).  Where there are
+// fewer shares than loads the rest are not made (12020 rows of 80 in 3 shares: 4 us less than with one share read again and again).
 template <bool BF16, int LANES, int WAVES>
 __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs g)
 {
@@ -27,19 +28,20 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs g)
     const float *ml = g.part_ml + 2 * row * g.splits, *po = g.part_o + row * g.splits * g.D + (d < g.D ? d : 0);
     float m = -INFINITY, l = 0.f;
     float4v o{0.f, 0.f, 0.f, 0.f};
-    for (int s0 = part; s0 < g.splits; s0 += PARTS * AT_ONCE) {
+    for (int s0 = 0; s0 < g.splits; s0 += PARTS * AT_ONCE) {
         float2v f[AT_ONCE];
         float4v x[AT_ONCE];
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i) {
-            const int s = s0 + i * PARTS < g.splits ? s0 + i * PARTS : s0;
+            if (s0 + i * PARTS >= g.splits) continue;                      // (wavefront-uniform)
+            const int s = s0 + i * PARTS + part < g.splits ? s0 + i * PARTS + part : g.splits - 1;
             __builtin_memcpy(&f[i], ml + 2 * s, 8);
             __builtin_memcpy(&x[i], po + (int64_t)s * g.D, 16);
         }
         float top = m;
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i) {
-            if (i && s0 + i * PARTS >= g.splits) f[i] = float2v{-INFINITY, 0.f};
+            if (s0 + i * PARTS + part >= g.splits) f[i] = float2v{-INFINITY, 0.f};
             top = fmaxf(top, f[i][0]);
         }
         const float ref = top == -INFINITY ? 0.f : top, old = __builtin_amdgcn_exp2f(m - ref);
@@ -48,7 +50,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(const PagedArgs g)
         o = o * old;
 #pragma unroll
         for (int i = 0; i < AT_ONCE; ++i) {
-            if (i && s0 + i * PARTS >= g.splits) continue;                 // (what is there once more may be an infinity)
+            if (s0 + i * PARTS + part >= g.splits) continue;               // (what is there once more may be an infinity)
             const float w = __builtin_amdgcn_exp2f(f[i][0] - ref);
             l = __builtin_fmaf(f[i][1], w, l);
 #pragma unroll
@@ -156,7 +158,8 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     a.causal = causal ? 1 : 0;
     a.window = (int32_t)std::min<int64_t>(window, 1 << 30);
     const int64_t es = kind == CACHE_SAME ? 2 : 1, most_bytes = (1LL << 31) - 4096;
-    a.uniform = page_size % 16 == 0 && a.k_ss >= 0 && a.k_ss < most_bytes / (16 * es) && a.v_ss >= 0 && a.v_ss < most_bytes / (16 * es);
+    a.near = a.k_ss >= 0 && a.k_ss < most_bytes / (16 * es) && a.v_ss >= 0 && a.v_ss < most_bytes / (16 * es);
+    a.uniform = a.near && page_size % 16 == 0;
     a.aligned = (((uintptr_t)a.K | (uintptr_t)a.V | (uint64_t)((a.k_sp | a.k_ss | a.k_sh | a.v_sp | a.v_ss | a.v_sh) * es)) & 15) == 0;
     a.page = divider_of((uint32_t)page_size);
     a.group = divider_of((uint32_t)a.G);
@@ -177,8 +180,8 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     const int64_t block = rows == kManyRows ? many_keys(built) : few_trip(kind, built);
     int64_t splits;
     if (rows == kManyRows) {
-        // Two programs for a unit, of 192 keys each and more (us, graph replays, 32/8 heads x 128 bf16: 64 queries x 600 keys 21.6 unshared, 15.8 in 3 shares,
-        // 1000 29.9 / 17.9 in 4, 20000 526 / 49.5 in 32; 200 x 4000 109 / 38.4 in 8, 60.3 in 16; 7 x 200 in windows of 512 32.0 / 32.9 in 3).
+        // Two programs for a unit, of 192 keys each and more (us, graph replays, 32/8 heads x 128 bf16: 64 queries x 600 keys 22 unshared, 15.1 in 3 shares,
+        // 1000 30 / 17.2 in 4, 20000 526 / 49.5 in 32; 200 x 4000 109 / 38.4 in 8, 60.3 in 16; 7 x 200 in windows of 512 29.6 / 29.1 in 3).
         splits = std::min(base >= 256 ? 1 : 512 / base, length / 192);
     } else {
         // As many programs as units, of 48 KB of K and V and more each (us, graph replays: 1 x 8 heads x 128 bf16, 500 keys 12.0 unshared, 9.5 in 6 shares, 2000 32.3 / 10.7

@@ -31,12 +31,15 @@ template <int SIZE, bool BF16, int KIND>
 static nt_status launch_paged_kind(const PagedArgs &a, int rows, int64_t programs, hipStream_t s)
 {
     static_assert(kFewWaves == 4 && kManyWaves == 4, "256 threads");
-    static DeviceOnce many[2];
+    static DeviceOnce many[3];
     if (rows == 16) return launch_paged_few<SIZE, BF16, KIND, 1>(a, programs, s);
     if constexpr (SIZE < 256)                                              // (two sets of 16 rows of 256 elements do not fit the registers)
         if (rows == 32) return launch_paged_few<SIZE, BF16, KIND, 2>(a, programs, s);
-    if (a.uniform && a.aligned && a.D == SIZE) return launch_paged_inst(paged_many_kernel<BF16, KIND, SIZE, true>, many[0], "paged_many_kernel", many_lds(SIZE), a, programs, s);
-    return launch_paged_inst(paged_many_kernel<BF16, KIND, SIZE, false>, many[1], "paged_many_kernel", many_lds(SIZE), a, programs, s);
+    const bool together = a.near && a.aligned && a.page.d % many_together(KIND, SIZE) == 0 && a.D % many_piece(KIND) == 0;
+    const char *name = "paged_many_kernel";
+    if (together && a.D == SIZE) return launch_paged_inst(paged_many_kernel<BF16, KIND, SIZE, true, true>, many[0], name, many_lds(SIZE), a, programs, s);
+    if (together) return launch_paged_inst(paged_many_kernel<BF16, KIND, SIZE, true, false>, many[1], name, many_lds(SIZE), a, programs, s);
+    return launch_paged_inst(paged_many_kernel<BF16, KIND, SIZE, false, false>, many[2], name, many_lds(SIZE), a, programs, s);
 }
 
 // rows: to a program, 16, 32 (paged_few_kernel) or kManyRows

@@ -7,9 +7,9 @@
 // sees are not computed.  With an 8-bit cache the codes are widened on their way to LDS, a key's scale multiplies its scores in fp32 and a value's scale
 // its weight, so that nothing is rounded but the weights, as in a 16-bit cache.
 //
-// FAST (whole rows at addresses that are multiples of 16 bytes, pages of a multiple of 16 keys): the rows that a wavefront moves with one load lie on one page; the table is read and the addresses are
-// made by one lane for all.  A 16-bit cache then travels straight into LDS, one block ahead, codes through registers, 16 at a time.  Other caches: 8
-// elements to a lane through registers, every lane with an address of its own.
+// FAST (rows at addresses that are multiples of 16 bytes, and pages that hold the 2 to 16 rows that a wavefront moves with one load or a multiple of
+// them, so that these lie on one page): the table is read and the addresses are made by one lane for all.  A 16-bit cache then travels straight into
+// LDS, one block ahead, codes through registers, 16 at a time.  Other caches: 8 elements to a lane through registers, every lane with an address of its own.
 #pragma once
 #include "paged.h"
 
@@ -17,15 +17,19 @@ namespace nt {
 
 constexpr int kManyWaves = 4, kManyRows = 32 * kManyWaves;
 constexpr int many_keys(int size) { return size == 256 ? 32 : 64; }
+// elements that a lane moves at a time (FAST), and the rows that a wavefront then moves with one load
+constexpr int many_piece(int kind) { return kind == CACHE_SAME ? 8 : 16; }
+constexpr int many_together(int kind, int size) { return 64 * many_piece(kind) / size; }
 constexpr size_t many_block(int size) { return (size_t)many_keys(size) * size * 2; }
 // [K0][K1][V0][V1], scales of two blocks (K's, then V's), three flags
 constexpr size_t many_lds(int size) { return 4 * many_block(size) + 2 * 2 * many_keys(size) * 4 + 16; }
 
-template <bool BF16, int KIND, int SIZE, bool FAST>
+// FULL: rows of SIZE elements (the switched-off lanes of others cost 5 % where none is: 1024 queries x 8000 keys x 32/8 heads x 128 bf16 216 us, 228)
+template <bool BF16, int KIND, int SIZE, bool FAST, bool FULL>
 __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 : 1) void paged_many_kernel(const PagedArgs g)
 {
     constexpr bool DMA = FAST && KIND == CACHE_SAME;
-    constexpr int EPL = FAST && KIND != CACHE_SAME ? 16 : 8;               // elements that a lane moves at a time
+    constexpr int EPL = FAST ? many_piece(KIND) : 8;
     constexpr int KB = many_keys(SIZE), JB = KB / 32, CH = SIZE / EPL, PER = KB * CH / 256, RSTEP = 256 / CH;
     constexpr int ES = KIND == CACHE_SAME ? 2 : 1;
     constexpr uint32_t BLK = many_block(SIZE);
@@ -106,7 +110,11 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
     // rows that lie 8 apart (head size 256) the order of the pieces differs in its last bit.
     const int lane_row = FAST ? lane / CH : 0;
     const uint32_t at_piece = DMA ? (uint32_t)(lane % CH) ^ chunk_order<SIZE>((uint32_t)(wave * (RSTEP / 4) + lane_row)) : (uint32_t)(lane % CH);
-    const uint32_t kl = FAST ? (uint32_t)(lane_row * (int32_t)g.k_ss * ES) + 16 * at_piece : 0, vl = FAST ? (uint32_t)(lane_row * (int32_t)g.v_ss * ES) + 16 * at_piece : 0;
+    // (codes beyond the head size: the row's last ones, see stash; 16-bit elements beyond it are not fetched)
+    const uint32_t piece = DMA || FULL || at_piece < (uint32_t)g.D / EPL ? at_piece : (uint32_t)g.D / EPL - 1;
+    const uint32_t kl = FAST ? (uint32_t)(lane_row * (int32_t)g.k_ss * ES) + 16 * piece : 0, vl = FAST ? (uint32_t)(lane_row * (int32_t)g.v_ss * ES) + 16 * piece : 0;
+    // whether the lane's piece of the wavefront's row u holds elements (DMA; at head size 256 odd u have the pieces in another order)
+    auto holds = [&](int u) { return FULL || 8 * (at_piece ^ (uint32_t)(RSTEP == 8 && (u & 1))) < (uint32_t)g.D; };
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
     auto fetch = [&](int kb, uint32_t copy) {
         named = 0;
@@ -129,13 +137,30 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
             const uint64_t p = reinterpret_cast<uint64_t>(address[0][0]);
             return reinterpret_cast<const char *>((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)p, l) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(p >> 32), l) << 32);
         };
+        if constexpr (DMA) {
+            const uint32_t to = lds0 + copy * BLK + (uint32_t)(wave * (RSTEP / 4) * SIZE * 2);
+            auto flip = [&](int u) { return RSTEP == 8 && (u & 1) ? (at_piece & 1 ? 0u - 16u : 16u) : 0u; };
+            if constexpr (FULL) {
 #pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            if constexpr (DMA) {
-                const uint32_t flip = RSTEP == 8 && (u & 1) ? (at_piece & 1 ? 0u - 16u : 16u) : 0u, to = lds0 + copy * BLK + (uint32_t)((u * RSTEP + wave * (RSTEP / 4)) * SIZE * 2);
-                dma16(of_lane(u), kl + flip, to);
-                dma16(of_lane(PER + u), vl + flip, to + 2 * BLK);
-            } else if constexpr (FAST) {
+                for (int u = 0; u < PER; ++u) {
+                    dma16(of_lane(u), kl + flip(u), to + (uint32_t)(u * RSTEP * SIZE * 2));
+                    dma16(of_lane(PER + u), vl + flip(u), to + (uint32_t)(u * RSTEP * SIZE * 2) + 2 * BLK);
+                }
+            } else {
+                const char *from[2 * PER];                                 // (in scalar registers before lanes are switched off)
+#pragma unroll
+                for (int u = 0; u < 2 * PER; ++u) from[u] = of_lane(u);
+#pragma unroll
+                for (int u = 0; u < PER; ++u)
+                    if (holds(u)) {
+                        dma16(from[u], kl + flip(u), to + (uint32_t)(u * RSTEP * SIZE * 2));
+                        dma16(from[PER + u], vl + flip(u), to + (uint32_t)(u * RSTEP * SIZE * 2) + 2 * BLK);
+                    }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < (DMA ? 0 : PER); ++u) {
+            if constexpr (FAST) {
                 __builtin_memcpy(&kr[u], of_lane(u) + kl, 16);
                 __builtin_memcpy(&vr[u], of_lane(PER + u) + vl, 16);
             } else {
@@ -163,7 +188,7 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
                 for (int u = 0; u < PER; ++u) {
                     const int32_t r = u * RSTEP + wave * (RSTEP / 4) + here(lane) / CH, key = kb * KB + r;
                     const uint32_t at = copy * BLK + (uint32_t)((u * RSTEP + wave * (RSTEP / 4)) * SIZE * 2 + here(lane) * 16);
-                    if (!((named >> u) & 1)) lds_write16(smem, at, u32x4{kNanPair, kNanPair, kNanPair, kNanPair});
+                    if (!((named >> u) & 1) && holds(u)) lds_write16(smem, at, u32x4{kNanPair, kNanPair, kNanPair, kNanPair});
                     if (!((named >> u) & 1) || key < keys.lo || key >= keys.hi) lds_write16(smem, at + 2 * BLK, u32x4{0, 0, 0, 0});
                     else if (hidden) odd = odd | any_not_finite<BF16>(lds_read16(smem, at + 2 * BLK));
                 }
@@ -189,7 +214,7 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
                         k = widen8<BF16, KIND>(u32x2{kr[u][0], kr[u][1]});
                         v = widen8<BF16, KIND>(u32x2{vr[u][0], vr[u][1]});
                     }
-                    if (!FAST && 8 * ch >= g.D) k = v = u32x4{0, 0, 0, 0};
+                    if (!FULL && EPL * ch >= g.D) k = v = u32x4{0, 0, 0, 0};
                     k = page ? k : u32x4{kNanPair, kNanPair, kNanPair, kNanPair};
                     v = good ? v : u32x4{0, 0, 0, 0};
                     if (hidden) odd = odd | any_not_finite<BF16>(v);
@@ -413,6 +438,8 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
     const int k_end = keys.lo < keys.hi ? (keys.hi + KB - 1) / KB : 0;
     int kb = keys.lo < keys.hi ? keys.lo / KB : 0;
     if (tid < 3) flags[tid] = 0;
+    if (DMA && !FULL)                                                      // what no load writes
+        for (uint32_t i = here(tid); i < 4 * BLK / 16; i += 256) lds_write16(smem, 16 * i, u32x4{0, 0, 0, 0});
     __syncthreads();
     if (kb < k_end) {                                                      // (workgroup-uniform, as the loop's count)
         find(kb);

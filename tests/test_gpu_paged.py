@@ -236,6 +236,21 @@ def test_pages_of_whole_groups_of_keys(dt, kind, size, layout):
 
 
 @pytest.mark.parametrize("dt,kind", KINDS)
+@pytest.mark.parametrize("size,page", [(8, 8), (40, 24), (48, 16), (72, 4), (80, 24), (96, 12), (112, 8), (136, 2), (192, 4), (248, 6), (128, 4), (256, 2), (64, 8), (64, 24), (128, 1)])
+def test_sizes_between_and_pages_of_few_keys(dt, kind, size, page):
+    """Chunks, with head sizes below the next built one and pages that hold a few of the rows that are fetched together, or none."""
+    seqs = [(70, 150), (1, 97), (33, 33), (130, 131)]
+    b = attend(seqs, 2, 2, size, page, dt, kind, seed=8, plan=(128, None))
+    want = b.run().clone()
+    b.table[0, 100 // page] = -1                                              # of the first sequence: keys that its last 50 tokens or more see
+    got = b.run()
+    b.check(got)
+    first = 100 // page * page - 80
+    assert torch.equal(got[:first], want[:first]) and torch.isnan(got[first + page:70]).all() and torch.equal(got[70:], want[70:])
+
+
+
+@pytest.mark.parametrize("dt,kind", KINDS)
 def test_shared_keys(dt, kind):
     """Long pasts and few programs: shares, their ends inside and beyond the shorter sequences."""
     attend([(1, 4000), (1, 5), (1, 1800), (1, 0)], 8, 2, 128, 16, dt, kind, hints=(1, 4000), plan=(16, True))
