@@ -5,7 +5,8 @@
 // with up12 rounding up to twelve significant bits, s at least 2^-100, and at most what keeps L s in fp16's range for fp16 tokens; reading gives
 // code * s, rounded to 16 bits.  Rounded up, s never makes a code larger than L; and short, it leaves nothing between the quotient's border cases to
 // be lost in 32 bits: a border t (the middle between two codes) has at most 8 significant bits, t s at most 20, x at most 11, so x / s is t exactly or
-// differs from it by 2^-20 and more, far beyond the 2^-23 that the arithmetic may be off.  The codes are those of the real quotient, and code * s (8 x 12 bits) is exact in 32 bits.
+// differs from it by 2^-20 and more, far beyond the 2^-23 that the arithmetic may be off.  The codes are those of the
+// real quotient, and code * s (8 x 12 bits) is exact in 32 bits.
 // A row with an infinity or NaN has no scale: s is NaN, its codes are 0, and it reads as NaN.
 //
 // Both are bound by memory: a row's elements once in 16 bits and once as they are held.  A group of 8, 16 or 32 lanes has a row, 8 elements to a lane (16

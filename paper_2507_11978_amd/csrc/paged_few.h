@@ -10,6 +10,9 @@
 // K goes from memory straight into the operand's registers (a lane holds its key's elements).  V has to be turned: through registers into LDS, a region per
 // wavefront, and out with transposing reads; no barrier in the loop.  A trip takes as many tiles as make 16 KB of K and V, all of them in flight at once: K's
 // loads for the next trip go out once the scores are there, V's as its registers empty into LDS.
+//
+// Bound by reading K and V: 64 sequences of 17 to 4096 tokens, 32/8 heads x 128 bf16 134 us = 4.15 TB/s (a large copy reaches 4.84), 2 of 131072 in e4m3 128 us =
+// 4.3 TB/s, 32 of 2047 with 48 heads x 64 in int8 62.5 us = 4.6 TB/s; one of 900 12.5 us, most of it the host's call and one wavefront's chain of loads.
 #pragma once
 #include "paged.h"
 
