@@ -11,8 +11,8 @@
 // them, so that these lie on one page): the table is read and the addresses are made by one lane for all.  A 16-bit cache then travels straight into
 // LDS, one block ahead, codes through registers, 16 at a time.  Other caches: 8 elements to a lane through registers, every lane with an address of its own.
 //
-// Measured: 2048 queries of 32/8 heads x 128 bf16 over 18500 keys 640 us = 0.91 PFLOP/s (a large matrix product reaches 1.18), 1024 queries x 8000 216, over
-// e4m3 340, int8 354 (each lane widens 64 elements of a block and scales 64 scores and weights).  A block of 64 keys is 32 matrix instructions of 32 cycles and 4 of 16 to a wavefront beside 32 exponentials, the multiplications and packs
+// Measured: 2048 queries of 32/8 heads x 128 bf16 over 18500 keys 628 us = 0.93 PFLOP/s (a large matrix product reaches 1.18), 1024 queries x 8000 214, over
+// e4m3 315, int8 328 (each lane widens 64 elements of a block and scales 64 scores and weights).  A block of 64 keys is 32 matrix instructions of 32 cycles and 4 of 16 to a wavefront beside 32 exponentials, the multiplications and packs
 // that feed them; the matrix pipe is busy for 36 % of the cycles, LDS has no conflicts.  Two wavefronts to a SIMD (128; three at 64) are what the registers
 // allow, and where both weigh their blocks the pipe waits.  Tried: the next block's products between this block's exponentials (K two blocks ahead, two
 // sets of scores): 629 us with all 256 registers, but 7.5 % slower at head size 64 and half again as long where registers ran out; blocks of 32 keys: 775.
@@ -30,7 +30,7 @@ constexpr size_t many_block(int size) { return (size_t)many_keys(size) * size * 
 // [K0][K1][V0][V1], scales of two blocks (K's, then V's), three flags
 constexpr size_t many_lds(int size) { return 4 * many_block(size) + 2 * 2 * many_keys(size) * 4 + 16; }
 
-// FULL: rows of SIZE elements (the switched-off lanes of others cost 5 % where none is: 1024 queries x 8000 keys x 32/8 heads x 128 bf16 216 us, 228)
+// FULL: rows of SIZE elements (the switched-off lanes of others cost 5 % where none is: 1024 queries x 8000 keys x 32/8 heads x 128 bf16 217 us, 228)
 template <bool BF16, int KIND, int SIZE, bool FAST, bool FULL>
 __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 : 1) void paged_many_kernel(const PagedArgs g)
 {
@@ -285,13 +285,11 @@ __global__ __launch_bounds__(64 * kManyWaves, SIZE == 64 ? 3 : SIZE == 128 ? 2 :
         const bool hidden = base < all_lo || base + KB > all_hi;          // wavefront-uniform: from some row
         if (hidden) {
             const float out = g.scale_log2e >= 0.f ? -INFINITY : INFINITY;
+            const uint32_t from = here(base + 4 * hi) - row_lo, count = row_hi > row_lo ? row_hi - row_lo : 0;      // (keys before row_lo: far beyond count)
 #pragma unroll
             for (int jb = 0; jb < JB; ++jb)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const int32_t key = base + 32 * jb + 8 * (v / 4) + 4 * hi + (v % 4);
-                    if (key < row_lo || key >= row_hi) st[jb][v] = out;
-                }
+                for (int v = 0; v < 16; ++v) st[jb][v] = from + (uint32_t)(32 * jb + 8 * (v / 4) + v % 4) < count ? st[jb][v] : out;
         }
         if constexpr (NORM) {
             const float *vs = &scales[copy * 2 * KB + KB];
