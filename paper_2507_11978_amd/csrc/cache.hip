@@ -12,7 +12,7 @@
 // Both are bound by memory: a row's elements once in 16 bits and once as they are held.  A group of 8, 16 or 32 lanes has a row, 8 elements to a lane (16
 // bytes of either tensor: K's and V's rows go through the same lanes), the largest magnitude from exchanges within the group.  Measured: 16384 tokens
 // of 8 heads x 128 bf16 as int8 24.3 us written (4.15 TB/s), 18.6 read; 65536 read as e4m3 82 (4.9 TB/s, what a large copy reaches); calls of few tokens
-// take the host's 3 to 4 us, the kernel 2 to 3.
+// take the host's 3 to 4 us, the kernel 2 to 3 (a chain of launch, slot, row and store; dividing in 32 bits instead of 64 changes nothing).
 #include "paged.h"
 
 namespace nt {
@@ -94,12 +94,6 @@ __device__ __forceinline__ u32x2 quantise(u32x4 x, float *scale)
     return code;
 }
 
-// (a division in 64 bits is a fifth of a small call's time: one token of 8 heads x 128 written as e4m3 3.0 us on the GPU, so 2.4, read back 2.2, 1.8)
-__device__ __forceinline__ int64_t page_of(const CacheArgs &g, int64_t slot)
-{
-    return g.places >> 32 ? slot / g.page_size : (int64_t)((uint32_t)slot / (uint32_t)g.page_size);
-}
-
 template <bool BF16, int KIND, int LANES>
 __global__ __launch_bounds__(256) void cache_write_kernel(const CacheArgs g)
 {
@@ -116,7 +110,7 @@ __global__ __launch_bounds__(256) void cache_write_kernel(const CacheArgs g)
         __builtin_memcpy(&v, g.v + token * g.v_st + h * g.v_sh + d, 16);
     }
     if ((uint64_t)slot >= (uint64_t)g.places) return;
-    const int64_t page = page_of(g, slot), at = slot - page * g.page_size;
+    const int64_t page = slot / g.page_size, at = slot - page * g.page_size;
     constexpr int ES = KIND == CACHE_SAME ? 2 : 1;
     char *K = g.K + (page * g.ck_sp + at * g.ck_ss + h * g.ck_sh + d) * ES, *V = g.V + (page * g.cv_sp + at * g.cv_ss + h * g.cv_sh + d) * ES;
     if constexpr (KIND == CACHE_SAME) {
@@ -170,7 +164,7 @@ __global__ __launch_bounds__(256) void cache_read_kernel(const CacheArgs g)
     const int64_t slot = g.slots[token];
     u32x4 k{0, 0, 0, 0}, v{0, 0, 0, 0};
     if ((uint64_t)slot < (uint64_t)g.places) {
-        const int64_t page = page_of(g, slot), at = slot - page * g.page_size;
+        const int64_t page = slot / g.page_size, at = slot - page * g.page_size;
         constexpr int ES = KIND == CACHE_SAME ? 2 : 1;
         const char *K = g.K + (page * g.ck_sp + at * g.ck_ss + h * g.ck_sh + d) * ES, *V = g.V + (page * g.cv_sp + at * g.cv_ss + h * g.cv_sh + d) * ES;
         if constexpr (KIND == CACHE_SAME) {

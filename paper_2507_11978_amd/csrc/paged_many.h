@@ -11,7 +11,7 @@
 // them, so that these lie on one page): the table is read and the addresses are made by one lane for all.  A 16-bit cache then travels straight into
 // LDS, one block ahead, codes through registers, 16 at a time.  Other caches: 8 elements to a lane through registers, every lane with an address of its own.
 //
-// Measured: 2048 queries of 32/8 heads x 128 bf16 over 18500 keys 628 us = 0.93 PFLOP/s (a large matrix product reaches 1.18), 1024 queries x 8000 214, over
+// Measured: 2048 queries of 32/8 heads x 128 bf16 over 18500 keys 628 to 645 us = 0.91 to 0.93 PFLOP/s (a large matrix product reaches 1.18), 1024 queries x 8000 214, over
 // e4m3 315, int8 328 (each lane widens 64 elements of a block and scales 64 scores and weights).  A block of 64 keys is 32 matrix instructions of 32 cycles
 // and 4 of 16 to a wavefront beside 32 exponentials, the multiplications and packs that feed them; the matrix pipe is busy for 36 % of the cycles, LDS has
 // no conflicts.  Two wavefronts to a SIMD (128; three at 64) are what the registers allow, and where both weigh their blocks the pipe waits.  Tried: the next block's products between this block's exponentials (K two blocks ahead, two
