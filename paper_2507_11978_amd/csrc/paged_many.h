@@ -378,7 +378,10 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
                 exponentials(m_ref == -INFINITY ? 0.f : m_ref);
                 if constexpr (KIND == CACHE_SAME) rs = matrix_sum(true);
                 keep = m_ref != -INFINITY && rs < 32768.f;
-                if constexpr (KIND != CACHE_SAME) keep = keep && __shfl_xor(rs, 32, 64) < 32768.f;
+                if constexpr (KIND != CACHE_SAME) {
+                    const float other = __shfl_xor(rs, 32, 64);            // the row's other lane (exchanged by all: a lane that is switched off reads as 0)
+                    keep = keep && other < 32768.f;
+                }
             }
             float mx = -INFINITY;
 #pragma unroll
