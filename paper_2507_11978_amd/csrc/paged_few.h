@@ -345,9 +345,13 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
 #pragma unroll
                         for (int v = 0; v < 4; ++v) p[4 * u + v] *= NORM ? v4[v] * per_unit[mb] : v4[v];
                     }
-                    if (!clear) {                                          // (the scale of a hidden key may be anything)
+                    if (!clear) {                                          // (the scale of a hidden key may be anything; a seen one's NaN shows whatever its weight)
+                        const int32_t first = here(base + 4 * g4);
 #pragma unroll
-                        for (int j = 0; j < 4 * NG; ++j) p[j] = s[j] == -INFINITY ? 0.f : p[j];
+                        for (int j = 0; j < 4 * NG; ++j) {
+                            const int32_t key = first + 16 * (j / 4) + j % 4;
+                            p[j] = key >= row_lo[mb] && key < row_hi[mb] ? p[j] : 0.f;
+                        }
                     }
                 }
 #pragma unroll

@@ -339,11 +339,7 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
                             sum += (p[0] + p[1]) + (p[2] + p[3]);
                             const float4v v4 = *reinterpret_cast<const float4v *>(&scales[copy * 2 * KB + KB + 32 * jb + 16 * s2 + 8 * q + 4 * hi]);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                const float x = p[e] * (NORM ? v4[e] * per_unit : v4[e]);
-                                // (the scale of a hidden key may be anything; that of a seen one with a weight of 0 hides no NaN either way)
-                                p[e] = hidden && p[e] == 0.f ? 0.f : x;
-                            }
+                            for (int e = 0; e < 4; ++e) p[e] *= NORM ? v4[e] * per_unit : v4[e];
                         }
                         pk[jb][s2][2 * q] = pack_two<BF16>(p[0], p[1]);
                         pk[jb][s2][2 * q + 1] = pack_two<BF16>(p[2], p[3]);
@@ -402,6 +398,14 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
             pending = __any(m_new == -INFINITY);
         }
         l_run += rs;
+        if (KIND != CACHE_SAME && hidden) {                                // (the scale of a hidden key may be anything; a seen one's NaN shows whatever its weight)
+            const uint32_t from = here(base + 4 * hi) - row_lo, count = row_hi > row_lo ? row_hi - row_lo : 0;
+#pragma unroll
+            for (int i = 0; i < 8 * JB; ++i) {                             // pair i: key 8 (i / 2) + 4 hi + 2 (i % 2) of the block and the next
+                const uint32_t j = from + (uint32_t)(8 * (i / 2) + 2 * (i % 2));
+                pk[i / 8][i / 4 % 2][i % 4] &= (j < count ? 0xffffu : 0u) | (j + 1 < count ? 0xffff0000u : 0u);
+            }
+        }
     };
     // ---- O^T += V^T P^T: k step (jb, s2) lists its 16 keys as 32 jb + 16 s2 + 8 part + 4 hi + 0 .. 3
     auto add_values = [&](const uint32_t copy) __attribute__((always_inline)) {
