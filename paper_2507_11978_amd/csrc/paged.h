@@ -100,6 +100,17 @@ __device__ __forceinline__ float widen_one(uint32_t w, int upper)
     else return (float)__builtin_bit_cast(_Float16, (uint16_t)h);
 }
 
+// What the rounding of two weights to `packed` left, packed alike.  fp16 queries over codes: a weight times a value's scale can be of any size beside its
+// neighbours', beyond fp16's range either way, so that codes, which bf16 holds exactly too, are multiplied in bf16.  One bf16 number would be off by 2^-9; the second
+// product runs with both parts and adds up what the weights themselves would give, to 2^-18 of them.  (Scales may be infinite: then nothing is left,
+// infinity less infinity is NaN.)
+template <bool BF16>
+__device__ __forceinline__ uint32_t rest_of(uint32_t packed, float a, float b)
+{
+    const float x = a - widen_one<BF16>(packed, 0), y = b - widen_one<BF16>(packed, 1);
+    return pack_two<BF16>(__builtin_fabsf(x) < INFINITY ? x : 0.f, __builtin_fabsf(y) < INFINITY ? y : 0.f);
+}
+
 // v if it is an infinity or NaN, else 0
 __device__ __forceinline__ float only_not_finite(float v) { return __builtin_fabsf(v) < INFINITY ? 0.f : v; }
 
@@ -147,13 +158,6 @@ __device__ __forceinline__ void wavefront_fence()
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
-// The power of two at or above a scale, kept where it and its reciprocal are normal numbers
-__device__ __forceinline__ float unit_above(float top)
-{
-    const uint32_t up = (__builtin_bit_cast(uint32_t, top) + 0x007fffffu) & 0x7f800000u;
-    return __builtin_bit_cast(float, up < 0x03800000u ? 0x03800000u : up > 0x7e000000u ? 0x7e000000u : up);
 }
 
 // a * s, 32 by 64 bits

@@ -37,7 +37,8 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
     constexpr int NV = KIND == CACHE_SAME ? SIZE / 32 : SIZE / 64;         // 16-byte loads per lane, 16 keys and tensor
     constexpr int ES = KIND == CACHE_SAME ? 2 : 1;
     constexpr int NT = few_tiles(KIND, SIZE), NG = 2 * NT, TRIP = 32 * NT;   // tiles of 32 and groups of 16 keys in a trip
-    constexpr bool NORM = KIND != CACHE_SAME && !BF16;                     // weights times scales may leave fp16's range: see `unit`
+    constexpr bool VB = BF16 || KIND != CACHE_SAME;                        // the second product's type is bf16,
+    constexpr bool SPLIT = VB && !BF16;                                    // ... where that is not the queries', with weights in two parts: see rest_of
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     __shared__ float red_m[kFewWaves][16 * MB], red_l[kFewWaves][16 * MB];
     __shared__ __attribute__((aligned(16))) float scales[KIND == CACHE_SAME ? 1 : kFewWaves][KIND == CACHE_SAME ? 4 : 2 * TRIP];     // K's, V's
@@ -187,11 +188,6 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
 #pragma unroll
             for (int db = 0; db < SIZE / 16; ++db) acc[mb][db] = float4v{0.f, 0.f, 0.f, 0.f};
         }
-        // NORM: a row's accumulator is held in units of a power of two that follows the largest scale it has seen, so that weight * scale / unit is at
-        // most 1 and in fp16's range whatever the size of the values
-        float unit[MB], per_unit[MB];
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb) unit[mb] = per_unit[mb] = 0.f;
 
         for (; t < t_end; t += kFewWaves) {
             const int base = t * TRIP, next = t + kFewWaves;
@@ -276,7 +272,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
             }
 
             // ---- weights
-            u32x4 pk[MB][NT];
+            u32x4 pk[MB][NT], rest[SPLIT ? MB : 1][NT];
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) {
                 float s[4 * NG];
@@ -317,33 +313,16 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
                     sum += p[j];
                 }
                 l[mb] = __builtin_fmaf(l[mb], alpha, sum);
-                float shrink = alpha;
-                if constexpr (NORM) {
-                    float most = 0.f;                                      // the largest scale that the row sees (fmax passes over NaN)
+                if (!__all(alpha == 1.f)) {
 #pragma unroll
-                    for (int u = 0; u < NG; ++u) {
-                        const float4v v4 = *reinterpret_cast<const float4v *>(&scales[wave][TRIP + 16 * u + 4 * g4]);
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) most = fmaxf(most, clear || s[4 * u + v] != -INFINITY ? __builtin_fabsf(v4[v]) : 0.f);
-                    }
-                    most = largest_across<true>(most);
-                    const float grown = most > unit[mb] ? unit_above(most) : unit[mb];
-                    if (grown != unit[mb]) {
-                        shrink *= unit[mb] == 0.f ? 0.f : unit[mb] / grown;
-                        unit[mb] = grown;
-                        per_unit[mb] = 1.f / grown;
-                    }
-                }
-                if (!__all(shrink == 1.f)) {
-#pragma unroll
-                    for (int db = 0; db < SIZE / 16; ++db) acc[mb][db] = acc[mb][db] * shrink;
+                    for (int db = 0; db < SIZE / 16; ++db) acc[mb][db] = acc[mb][db] * alpha;
                 }
                 if constexpr (KIND != CACHE_SAME) {
 #pragma unroll
                     for (int u = 0; u < NG; ++u) {
                         const float4v v4 = *reinterpret_cast<const float4v *>(&scales[wave][TRIP + 16 * u + 4 * g4]);
 #pragma unroll
-                        for (int v = 0; v < 4; ++v) p[4 * u + v] *= NORM ? v4[v] * per_unit[mb] : v4[v];
+                        for (int v = 0; v < 4; ++v) p[4 * u + v] *= v4[v];
                     }
                     if (!clear) {                                          // (the scale of a hidden key may be anything; a seen one's NaN shows whatever its weight)
                         const int32_t first = here(base + 4 * g4);
@@ -356,8 +335,12 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
                 }
 #pragma unroll
                 for (int i = 0; i < NT; ++i)
-                    pk[mb][i] = u32x4{pack_two<BF16>(p[8 * i], p[8 * i + 1]), pack_two<BF16>(p[8 * i + 2], p[8 * i + 3]), pack_two<BF16>(p[8 * i + 4], p[8 * i + 5]),
-                                      pack_two<BF16>(p[8 * i + 6], p[8 * i + 7])};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float a = p[8 * i + 2 * j], b = p[8 * i + 2 * j + 1];
+                        pk[mb][i][j] = pack_two<VB>(a, b);
+                        if constexpr (SPLIT) rest[mb][i][j] = rest_of<VB>(pk[mb][i][j], a, b);
+                    }
             }
             // ---- O^T += V^T P^T, 32 keys at a time: V into LDS (its registers take the next trip's), then lane (c16, g4) supplies d = 16 db + c16 and keys
             // 4 g4 + 0 .. 3, 16 + 4 g4 + 0 .. 3; lane i of a group of 16 points the transposing read at key i / 4 of its four, 8 bytes i % 4 of the 32
@@ -373,8 +356,8 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
                         if constexpr (KIND == CACHE_SAME) {
                             lds_write16(vt, lds_at<SIZE>(row, 4 * n + g4), x);
                         } else {
-                            lds_write16(vt, lds_at<SIZE>(row, 8 * n + 2 * g4), widen8<BF16, KIND>(u32x2{x[0], x[1]}));
-                            lds_write16(vt, lds_at<SIZE>(row, 8 * n + 2 * g4 + 1), widen8<BF16, KIND>(u32x2{x[2], x[3]}));
+                            lds_write16(vt, lds_at<SIZE>(row, 8 * n + 2 * g4), widen8<VB, KIND>(u32x2{x[0], x[1]}));
+                            lds_write16(vt, lds_at<SIZE>(row, 8 * n + 2 * g4 + 1), widen8<VB, KIND>(u32x2{x[2], x[3]}));
                         }
                     }
                     load_v(2 * i + u, more);
@@ -395,7 +378,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
                                 const bool sees = key >= row_lo[mb] && key < row_hi[mb];
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) {
-                                    const float x = only_not_finite(widen_one<BF16>(v[e >> 1], e & 1));
+                                    const float x = only_not_finite(widen_one<VB>(v[e >> 1], e & 1));
                                     acc[mb][db][e] += sees ? x : 0.f;
                                 }
                             }
@@ -404,7 +387,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
 #pragma unroll 1
                     for (int j = 0; j < SIZE / 16; ++j) {                  // (each lane has SIZE / 16 of the tile's 16-byte pieces)
                         const uint32_t at = lds_at<SIZE>(16 * (j & 1) + c, (j >> 1) * 4 + q);
-                        lds_write16(vt, at, without_not_finite<BF16>(lds_read16(vt, at)));
+                        lds_write16(vt, at, without_not_finite<VB>(lds_read16(vt, at)));
                     }
                     wavefront_fence();
                 }
@@ -425,11 +408,14 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
                     if (q + 1 < SIZE / 64) read_four(q + 1);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const u32x2 a = frag[q & 1][j][0], c = frag[q & 1][j][1];
+                    for (int part = 0; part < (SPLIT ? 2 : 1); ++part)
 #pragma unroll
-                        for (int mb = 0; mb < MB; ++mb) acc[mb][4 * q + j] = mfma16<BF16>(u32x4{a[0], a[1], c[0], c[1]}, pk[mb][i], acc[mb][4 * q + j]);
-                    }
+                        for (int j = 0; j < 4; ++j) {
+                            const u32x2 a = frag[q & 1][j][0], c = frag[q & 1][j][1];
+#pragma unroll
+                            for (int mb = 0; mb < MB; ++mb)
+                                acc[mb][4 * q + j] = mfma16<VB>(u32x4{a[0], a[1], c[0], c[1]}, part ? rest[mb][i] : pk[mb][i], acc[mb][4 * q + j]);
+                        }
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -449,11 +435,8 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
                 red_l[wave][16 * mb + lane16] = l[mb];
             }
 #pragma unroll
-            for (int db = 0; db < SIZE / 16; ++db) {
-                float4v v = acc[mb][db];
-                if constexpr (NORM) v = v * unit[mb];
-                *reinterpret_cast<float4v *>(ex + (16 * mb + lane16) * SIZE + 16 * db + 4 * lane4) = v;
-            }
+            for (int db = 0; db < SIZE / 16; ++db)
+                *reinterpret_cast<float4v *>(ex + (16 * mb + lane16) * SIZE + 16 * db + 4 * lane4) = acc[mb][db];
         }
         __syncthreads();
         for (int e = tid; e < 16 * MB * (SIZE / 4); e += 64 * kFewWaves) {

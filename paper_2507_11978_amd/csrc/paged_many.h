@@ -5,7 +5,8 @@
 // transposed, S^T = K Q^T with the query on the lane axis, weights against a reference M that lags behind the running maximum (raised when a
 // block holds a score 15 above it), packed weights as they are for O^T += V^T P^T.  Blocks that every row of a wavefront sees are not masked; those that none
 // sees are not computed.  With an 8-bit cache the codes are widened on their way to LDS, a key's scale multiplies its scores in fp32 and a value's scale
-// its weight, so that nothing is rounded but the weights, as in a 16-bit cache.
+// its weight, so that nothing is rounded but the weights, as in a 16-bit cache (fp16 queries: weights as two bf16 numbers, the second product twice: 20 us of the 365 that
+// 1024 queries x 8000 keys x 32/8 heads x 128 over e4m3 take).
 //
 // FAST (rows at addresses that are multiples of 16 bytes, and pages that hold the 2 to 16 rows that a wavefront moves with one load or a multiple of
 // them, so that these lie on one page): the table is read and the addresses are made by one lane for all.  A 16-bit cache then travels straight into
@@ -43,7 +44,8 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
     constexpr int KB = many_keys(SIZE), JB = KB / 32, CH = SIZE / EPL, PER = KB * CH / 256, RSTEP = 256 / CH;
     constexpr int ES = KIND == CACHE_SAME ? 2 : 1;
     constexpr uint32_t BLK = many_block(SIZE);
-    constexpr bool NORM = KIND != CACHE_SAME && !BF16;
+    constexpr bool VB = BF16 || KIND != CACHE_SAME;                        // the second product's type is bf16,
+    constexpr bool SPLIT = VB && !BF16;                                    // ... where that is not the queries', with weights in two parts: see rest_of
     constexpr int DEEP = 4;                                                // products that a fragment of K or V is read ahead of its own
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     float *const scales = reinterpret_cast<float *>(smem + 4 * BLK);
@@ -219,15 +221,15 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
                         v = vr[u];
                     } else if constexpr (FAST) {
                         k = widen8<BF16, KIND>(u32x2{kr[u][2 * half], kr[u][2 * half + 1]});
-                        v = widen8<BF16, KIND>(u32x2{vr[u][2 * half], vr[u][2 * half + 1]});
+                        v = widen8<VB, KIND>(u32x2{vr[u][2 * half], vr[u][2 * half + 1]});
                     } else {
                         k = widen8<BF16, KIND>(u32x2{kr[u][0], kr[u][1]});
-                        v = widen8<BF16, KIND>(u32x2{vr[u][0], vr[u][1]});
+                        v = widen8<VB, KIND>(u32x2{vr[u][0], vr[u][1]});
                     }
                     if (!FULL && EPL * ch >= g.D) k = v = u32x4{0, 0, 0, 0};
                     k = page ? k : u32x4{kNanPair, kNanPair, kNanPair, kNanPair};
                     v = good ? v : u32x4{0, 0, 0, 0};
-                    if (hidden) odd = odd | any_not_finite<BF16>(v);
+                    if (hidden) odd = odd | any_not_finite<VB>(v);
                     const uint32_t at = lds_at<SIZE>(r, EPL / 8 * ch + half);
                     lds_write16(smem, copy * BLK + at, k);
                     lds_write16(smem, (2 + copy) * BLK + at, v);
@@ -245,7 +247,6 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
 #pragma unroll
         for (int v = 0; v < 16; ++v) ot[db][v] = 0.f;
     float m_ref = -INFINITY, l_run = 0.f;                                  // reference (-inf: none yet) and sum (8-bit caches: of this lane's keys)
-    float unit = 0.f, per_unit = 0.f;                                      // of this lane's row, see paged_few.h
     bool pending = true;                                                   // wavefront-uniform: some row has no reference
     const uint32_t one_pair = ((lane >> 4) & 1) == ((lane >> 2) & 1) ? (BF16 ? 0x3f803f80u : 0x3c003c00u) : 0u;
     const u32x4 ones{one_pair, one_pair, one_pair, one_pair};              // (the sum of query lane % 32 in every lane: see attention.hip)
@@ -253,6 +254,7 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
     const uint32_t v_key = 4 * (gq >> 1) + (li >> 2), v_chunk = 2 * (gq & 1) + ((li >> 1) & 1), v_half = (li & 1) * 8;
 
     u32x4 pk[JB][2];                                                       // a block's weights, packed (8-bit caches: times the values' scales)
+    u32x4 rest[SPLIT ? JB : 1][2];                                         // ... and what their rounding left
     auto weigh = [&](const int kb, const uint32_t copy) __attribute__((always_inline)) {
         const int base = kb * KB;
         const char *ks_lds = smem + copy * BLK;
@@ -295,33 +297,6 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
 #pragma unroll
                 for (int v = 0; v < 16; ++v) st[jb][v] = from + (uint32_t)(32 * jb + 8 * (v / 4) + v % 4) < count ? st[jb][v] : out;
         }
-        if constexpr (NORM) {
-            const float *vs = &scales[copy * 2 * KB + KB];
-            float top = 0.f;                                               // the largest scale that the row sees
-            if (hidden) {
-#pragma unroll
-                for (int jb = 0; jb < JB; ++jb)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const int j = 32 * jb + 8 * (v / 4) + 4 * hi + (v % 4);
-                        if (base + j >= row_lo && base + j < row_hi) top = fmaxf(top, __builtin_fabsf(vs[j]));
-                    }
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
-            } else {
-                if (lane < KB) top = __builtin_fabsf(vs[lane]);
-#pragma unroll
-                for (int x = 1; x < 64; x <<= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
-            }
-            if (__any(top > unit)) {
-                const float grown = top > unit ? unit_above(top) : unit, shrink = unit == 0.f ? 0.f : unit / grown;
-                unit = grown;
-                per_unit = grown == 0.f ? 0.f : 1.f / grown;
-#pragma unroll
-                for (int db = 0; db < SIZE / 32; ++db)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) ot[db][v] *= shrink;
-            }
-        }
         // ---- weights and their sum
         float rs;
         auto exponentials = [&](const float m) {
@@ -339,10 +314,14 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
                             sum += (p[0] + p[1]) + (p[2] + p[3]);
                             const float4v v4 = *reinterpret_cast<const float4v *>(&scales[copy * 2 * KB + KB + 32 * jb + 16 * s2 + 8 * q + 4 * hi]);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) p[e] *= NORM ? v4[e] * per_unit : v4[e];
+                            for (int e = 0; e < 4; ++e) p[e] *= v4[e];
                         }
-                        pk[jb][s2][2 * q] = pack_two<BF16>(p[0], p[1]);
-                        pk[jb][s2][2 * q + 1] = pack_two<BF16>(p[2], p[3]);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const uint32_t w = pack_two<VB>(p[2 * i], p[2 * i + 1]);
+                            pk[jb][s2][2 * q + i] = w;
+                            if constexpr (SPLIT) rest[jb][s2][2 * q + i] = rest_of<VB>(w, p[2 * i], p[2 * i + 1]);
+                        }
                     }
             if constexpr (KIND != CACHE_SAME) rs = sum;
         };
@@ -403,7 +382,9 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
 #pragma unroll
             for (int i = 0; i < 8 * JB; ++i) {                             // pair i: key 8 (i / 2) + 4 hi + 2 (i % 2) of the block and the next
                 const uint32_t j = from + (uint32_t)(8 * (i / 2) + 2 * (i % 2));
-                pk[i / 8][i / 4 % 2][i % 4] &= (j < count ? 0xffffu : 0u) | (j + 1 < count ? 0xffff0000u : 0u);
+                const uint32_t seen = (j < count ? 0xffffu : 0u) | (j + 1 < count ? 0xffff0000u : 0u);
+                pk[i / 8][i / 4 % 2][i % 4] &= seen;
+                if constexpr (SPLIT) rest[i / 8][i / 4 % 2][i % 4] &= seen;
             }
         }
     };
@@ -423,7 +404,8 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < PRODUCTS; ++i) {
-            ot[i % DB] = mfma32<BF16>(f[i % DEEP], pk[i / DB / 2][i / DB % 2], ot[i % DB]);
+            ot[i % DB] = mfma32<VB>(f[i % DEEP], pk[i / DB / 2][i / DB % 2], ot[i % DB]);
+            if constexpr (SPLIT) ot[i % DB] = mfma32<VB>(f[i % DEEP], rest[i / DB / 2][i / DB % 2], ot[i % DB]);
             if (i + DEEP < PRODUCTS) f[i % DEEP] = fragment(i + DEEP);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -443,7 +425,7 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
                     __builtin_memcpy(&v, vs_lds + lds_at<SIZE>(j, 4 * db + q) + half * 8, 8);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float x = only_not_finite(widen_one<BF16>(v[e >> 1], e & 1));
+                        const float x = only_not_finite(widen_one<VB>(v[e >> 1], e & 1));
                         ot[db][4 * q + e] += sees ? x : 0.f;
                     }
                 }
@@ -479,7 +461,7 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
             __syncthreads();
             for (int i = here(tid); i < KB * (SIZE / 8); i += 256) {       // ... and taken out of the block
                 const uint32_t at = (2 + copy) * BLK + 16 * i;
-                lds_write16(smem, at, without_not_finite<BF16>(lds_read16(smem, at)));
+                lds_write16(smem, at, without_not_finite<VB>(lds_read16(smem, at)));
             }
             __syncthreads();
         }
@@ -491,7 +473,7 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
 
     // ---- O = O^T / l, stored along d: after the half-wavefronts trade register groups a lane owns d = 32 db + 16 hi .. + 15 of its row
     const float total = KIND == CACHE_SAME ? l_run : l_run + __shfl_xor(l_run, 32, 64);
-    const float factor = (g.splits > 1 ? 1.f : total == 0.f ? 0.f : 1.0f / total) * (NORM ? unit : 1.f);
+    const float factor = g.splits > 1 ? 1.f : total == 0.f ? 0.f : 1.0f / total;
     const int64_t at = (token * g.Hq + head) * g.splits + split;
     if (g.splits > 1 && real && hi == 0) *reinterpret_cast<float2v *>(g.part_ml + 2 * at) = float2v{m_ref, total};
 #pragma unroll
