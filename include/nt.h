@@ -369,9 +369,9 @@ nt_status nt_cache_read(const nt_paged_cache *cache, void *k, const nt_tensor_de
  * nothing with a score above -inf, gets zeros.  A token that sees a position whose page the table does not name (an entry outside the
  * cache, such as -1, or a position past the table's last entry) gets NaN.  Rows of q that belong to no sequence are passed over.  scale = 0
  * stands for 1 / sqrt(head_size).  out must not alias an input.
- * Scores, weights' sums and accumulators are fp32, the weights are rounded to `dtype` before they multiply V.  Over an 8-bit cache K's scale
- * multiplies the score and V's the weight, in fp32; that product multiplies V's codes as a bf16 number, for NT_F16 as the sum of two, which is off by
- * 2^-18 of it at most, however large or small the scales are beside each other.
+ * Scores, weights' sums and accumulators are fp32.  Over an 8-bit cache K's scale multiplies the score and V's the weight, in fp32.  What multiplies V then
+ * is the weight as the sum of two numbers of `dtype` (bf16 over codes), off by 2^-17 of it at most (fp16: 2^-23, or 2^-25 of a weight of 1), where a
+ * program has 16 or 32 rows, and over codes with NT_F16; otherwise, in whole chunks, as one number, off by half a step of the type (bf16 2^-8, fp16 2^-11).
  * max_queries, max_length: the most new tokens and the greatest length of a sequence, if the host knows them (0: it does not); they choose the
  * kernel and how the keys are shared out, so a bound that is too low costs time, not results.
  * Memory: the keys of long sequences are shared out over programs where there are few of them; the shares pass through the library's

@@ -100,15 +100,19 @@ __device__ __forceinline__ float widen_one(uint32_t w, int upper)
     else return (float)__builtin_bit_cast(_Float16, (uint16_t)h);
 }
 
-// What the rounding of two weights to `packed` left, packed alike.  fp16 queries over codes: a weight times a value's scale can be of any size beside its
-// neighbours', beyond fp16's range either way, so that codes, which bf16 holds exactly too, are multiplied in bf16.  One bf16 number would be off by 2^-9; the second
-// product runs with both parts and adds up what the weights themselves would give, to 2^-18 of them.  (Scales may be infinite: then nothing is left,
-// infinity less infinity is NaN.)
-template <bool BF16>
+// What the rounding of two weights to `packed` left, packed alike.  The second product runs with both and adds up what the weights themselves would give, to
+// 2^-17 of them in bf16, to 2^-23, or 2^-25 of a weight of 1, in fp16; one rounding is off by 2^-8 (2^-11), an error as large as that of the rounded result.
+// SCALED: a weight times a value's scale.  That can be of any size beside its neighbours', beyond fp16's range either way, so that codes, which bf16 holds
+// exactly too, are multiplied in bf16 whatever the queries' type.  (Scales may be infinite: then nothing is left, infinity less infinity is NaN.)
+template <bool BF16, bool SCALED>
 __device__ __forceinline__ uint32_t rest_of(uint32_t packed, float a, float b)
 {
-    const float x = a - widen_one<BF16>(packed, 0), y = b - widen_one<BF16>(packed, 1);
-    return pack_two<BF16>(__builtin_fabsf(x) < INFINITY ? x : 0.f, __builtin_fabsf(y) < INFINITY ? y : 0.f);
+    float x = a - widen_one<BF16>(packed, 0), y = b - widen_one<BF16>(packed, 1);
+    if constexpr (SCALED) {
+        x = __builtin_fabsf(x) < INFINITY ? x : 0.f;
+        y = __builtin_fabsf(y) < INFINITY ? y : 0.f;
+    }
+    return pack_two<BF16>(x, y);
 }
 
 // v if it is an infinity or NaN, else 0

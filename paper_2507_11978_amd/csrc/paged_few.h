@@ -11,6 +11,10 @@
 // wavefront, and out with transposing reads; no barrier in the loop.  A trip takes as many tiles as make 16 KB of K and V, all of them in flight at once: K's
 // loads for the next trip go out once the scores are there, V's as its registers empty into LDS.
 //
+// Weights multiply V as the sum of two 16-bit numbers each (rest_of): the second half of the products hides behind the loads (64 x 4096 bf16 134 us either way, 2 x
+// 131072 e4m3 128 and 129), but for two sets of 16 rows over codes (8 x 8 queries x 4000 keys x 32/8 heads x 128 e4m3 30.7 us, 32.8).  Rounded once they would be off
+// by as much as the rounded result.
+//
 // Bound by reading K and V: 64 sequences of 17 to 4096 tokens, 32/8 heads x 128 bf16 134 us = 4.15 TB/s (a large copy reaches 4.84), 2 of 131072 in e4m3 128 us =
 // 4.3 TB/s, 32 of 2047 with 48 heads x 64 in int8 62.5 us = 4.6 TB/s; one of 900 12.5 us, most of it the host's call and one wavefront's chain of loads.
 #pragma once
@@ -37,8 +41,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
     constexpr int NV = KIND == CACHE_SAME ? SIZE / 32 : SIZE / 64;         // 16-byte loads per lane, 16 keys and tensor
     constexpr int ES = KIND == CACHE_SAME ? 2 : 1;
     constexpr int NT = few_tiles(KIND, SIZE), NG = 2 * NT, TRIP = 32 * NT;   // tiles of 32 and groups of 16 keys in a trip
-    constexpr bool VB = BF16 || KIND != CACHE_SAME;                        // the second product's type is bf16,
-    constexpr bool SPLIT = VB && !BF16;                                    // ... where that is not the queries', with weights in two parts: see rest_of
+    constexpr bool VB = BF16 || KIND != CACHE_SAME;                        // the second product's type is bf16 (see rest_of)
     extern __shared__ __attribute__((aligned(1024))) char smem[];
     __shared__ float red_m[kFewWaves][16 * MB], red_l[kFewWaves][16 * MB];
     __shared__ __attribute__((aligned(16))) float scales[KIND == CACHE_SAME ? 1 : kFewWaves][KIND == CACHE_SAME ? 4 : 2 * TRIP];     // K's, V's
@@ -272,7 +275,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
             }
 
             // ---- weights
-            u32x4 pk[MB][NT], rest[SPLIT ? MB : 1][NT];
+            u32x4 pk[MB][NT], rest[MB][NT];
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) {
                 float s[4 * NG];
@@ -339,7 +342,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
                     for (int j = 0; j < 4; ++j) {
                         const float a = p[8 * i + 2 * j], b = p[8 * i + 2 * j + 1];
                         pk[mb][i][j] = pack_two<VB>(a, b);
-                        if constexpr (SPLIT) rest[mb][i][j] = rest_of<VB>(pk[mb][i][j], a, b);
+                        rest[mb][i][j] = rest_of<VB, KIND != CACHE_SAME>(pk[mb][i][j], a, b);
                     }
             }
             // ---- O^T += V^T P^T, 32 keys at a time: V into LDS (its registers take the next trip's), then lane (c16, g4) supplies d = 16 db + c16 and keys
@@ -408,7 +411,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
                     if (q + 1 < SIZE / 64) read_four(q + 1);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int part = 0; part < (SPLIT ? 2 : 1); ++part)
+                    for (int part = 0; part < 2; ++part)
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const u32x2 a = frag[q & 1][j][0], c = frag[q & 1][j][1];

@@ -5,8 +5,11 @@
 // transposed, S^T = K Q^T with the query on the lane axis, weights against a reference M that lags behind the running maximum (raised when a
 // block holds a score 15 above it), packed weights as they are for O^T += V^T P^T.  Blocks that every row of a wavefront sees are not masked; those that none
 // sees are not computed.  With an 8-bit cache the codes are widened on their way to LDS, a key's scale multiplies its scores in fp32 and a value's scale
-// its weight, so that nothing is rounded but the weights, as in a 16-bit cache (fp16 queries: weights as two bf16 numbers, the second product twice: 20 us of the 365 that
-// 1024 queries x 8000 keys x 32/8 heads x 128 over e4m3 take).
+// its weight, so that nothing is rounded but the weights, as in a 16-bit cache.
+//
+// Weights are rounded to 16 bits once, and over 16-bit caches their sum is that of the rounded ones.  In two parts, as in paged_few.h, they would cost a second set of
+// products where products are the bound (1024 queries x 8000 keys x 32/8 heads x 128 bf16 212 us, 276 with two; 4 x 1024 x 48 heads x 64 f16 64, 98).  fp16 queries
+// over codes have no choice, see rest_of (20 us of the 365 that 1024 x 8000 e4m3 take).
 //
 // FAST (rows at addresses that are multiples of 16 bytes, and pages that hold the 2 to 16 rows that a wavefront moves with one load or a multiple of
 // them, so that these lie on one page): the table is read and the addresses are made by one lane for all.  A 16-bit cache then travels straight into
@@ -320,7 +323,7 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
                         for (int i = 0; i < 2; ++i) {
                             const uint32_t w = pack_two<VB>(p[2 * i], p[2 * i + 1]);
                             pk[jb][s2][2 * q + i] = w;
-                            if constexpr (SPLIT) rest[jb][s2][2 * q + i] = rest_of<VB>(w, p[2 * i], p[2 * i + 1]);
+                            if constexpr (SPLIT) rest[jb][s2][2 * q + i] = rest_of<VB, true>(w, p[2 * i], p[2 * i + 1]);
                         }
                     }
             if constexpr (KIND != CACHE_SAME) rs = sum;

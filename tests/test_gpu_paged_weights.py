@@ -3,7 +3,7 @@
 Bounds.  The result's rounding: h |O| with h = eps / 2 of its type (fp16: 2^-25 at least).  A score is an fp32 sum of `size` products, some eight more roundings
 follow until its exponential: off by 2^-24 (size + 8) S at most, with S the largest of scale * sum |q| |k| over the row's keys; that is the relative
 error of a weight, and twice that of the quotient.  Sums over n keys in fp32: 2^-24 (n + 16).  What the weights are rounded to before they multiply V: in two
-parts of bf16 2^-18 (the rest's rounding), in two of fp16 2^-22 and the spacing of its smallest numbers, 2^-25 of a weight of 1 for each key.
+parts of bf16 2^-17 (the rest's rounding; in the mean over a row's keys half of it at most, 2^-18), in two of fp16 2^-23 and the spacing of its smallest numbers, 2^-25 of a weight of 1 for each key.
 All of these but the first are relative to A = sum_j p_j |V_j|, the last to the largest |V|."""
 import numpy as np
 import pytest
@@ -11,7 +11,7 @@ import torch
 
 import paper_2507_11978_amd as nt
 from oracle import paged as op
-from test_gpu_paged import TORCH, Batch, f64, normal
+from test_gpu_paged import KINDS, TORCH, Batch, f64, normal
 
 pytestmark = pytest.mark.gpu
 
@@ -61,3 +61,17 @@ def test_a_large_value_that_weighs_nothing(kind, size, value, raised):
         torch.cuda.synchronize()
         assert nt.last_paged_plan().rows == (16 if hints else 128)
         check(b, got, f"{seqs} {at}")
+
+
+@pytest.mark.parametrize("dt,kind", KINDS)
+@pytest.mark.parametrize("q_heads,heads,size,page", [(1, 1, 64, 16), (8, 2, 128, 16), (6, 6, 80, 24), (4, 2, 256, 16), (20, 1, 120, 16)])
+def test_few_rows_round_the_result_only(dt, kind, q_heads, heads, size, page):
+    """One token of each sequence, or a few: reading K and V takes the time, the weights keep their bits."""
+    for seqs, length, shared in (([(1, 1), (1, 17), (1, 64), (1, 300)], 0, False), ([(1, 3000), (1, 40)], 3000, True)):
+        b = Batch(seqs, q_heads, heads, size, page, dt, kind, seed=2)
+        got = b.run(max_queries=1, max_length=length)
+        torch.cuda.synchronize()
+        p = nt.last_paged_plan()
+        held = length * size * 2 * (1 if kind in ("e4m3", "i8") else 2)       # of K and V to a head (shared from 384 KB on)
+        assert p.rows < 128 and (p.shares > 1) >= (shared and held >= 384 << 10)
+        check(b, got, f"{seqs}")
