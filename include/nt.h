@@ -367,7 +367,7 @@ nt_status nt_cache_read(const nt_paged_cache *cache, void *k, const nt_tensor_de
  *   j <= p if `causal`, and j > p - window if window > 0.
  * What a token does not see has no part in its result, whatever it holds.  A token that sees nothing (a length below the new tokens' count, or 0), or
  * nothing with a score above -inf, gets zeros.  A token that sees a position whose page the table does not name (an entry outside the
- * cache, such as -1, or a position past the table's last entry) gets NaN.  Rows of q that belong to no sequence are passed over.  scale = 0
+ * cache, such as -1, or a position past the table's last entry, or past 2^31 - 4097, which no table reaches) gets NaN.  Rows of q that belong to no sequence are passed over.  scale = 0
  * stands for 1 / sqrt(head_size).  out must not alias an input.
  * Scores, weights' sums and accumulators are fp32.  Over an 8-bit cache K's scale multiplies the score and V's the weight, in fp32.  What multiplies V then
  * is the weight as the sum of two numbers of `dtype` (bf16 over codes), off by 2^-17 of it at most (fp16: 2^-23, or 2^-25 of a weight of 1), where a

@@ -183,7 +183,7 @@ struct PagedArgs {
     int64_t t_sb;                      // sequence
     int32_t T, B, Hq, Hkv, G;          // tokens, sequences, heads, G = Hq / Hkv query heads to a key head
     int32_t D;                         // head size
-    int32_t width, pages;              // entries of a table row, pages of the cache
+    int32_t width, pages;              // entries of a table row (that are in reach), pages of the cache
     int32_t tiles;                     // of query rows, all sequences together (paged_many)
     int32_t causal, window;            // window 0: none
     int32_t near;                      // offsets within 16 rows of a page are not negative and fit 32 bits
@@ -200,7 +200,7 @@ __device__ __forceinline__ Sequence sequence_of(const PagedArgs &g, int b) { ret
 
 __device__ __forceinline__ KeyRange keys_of(const PagedArgs &g, const Sequence &q, int32_t i0, int32_t i1, int split, int32_t block)
 {
-    return key_range(q, i0, i1, g.causal, g.window, split, g.splits, g.split_keys, block);
+    return key_range(q, i0, i1, g.causal, g.window, split, g.splits, g.split_keys, block, g.width * (int32_t)g.page.d);
 }
 
 // ---- where a block of keys lies in LDS: rows of SIZE 16-bit elements, their 16-byte chunks in an order that depends on the row, such that 16

@@ -154,7 +154,7 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     }
     a.t_sb = W ? dt->stride[0] : 0;
     a.T = (int32_t)T; a.B = (int32_t)B; a.Hq = (int32_t)Hq; a.Hkv = (int32_t)Hkv; a.G = (int32_t)(Hq / Hkv); a.D = (int32_t)D;
-    a.width = (int32_t)W; a.pages = (int32_t)pages;
+    a.width = entries_in_reach(W, (uint32_t)page_size); a.pages = (int32_t)pages;
     a.causal = causal ? 1 : 0;
     a.window = (int32_t)std::min<int64_t>(window, 1 << 30);
     const int64_t es = kind == CACHE_SAME ? 2 : 1, most_bytes = (1LL << 31) - 4096;
@@ -174,7 +174,7 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     const int64_t base = (int64_t)a.tiles * Hkv;
     if (base > kMaxWorkgroups) return fail(NT_ERR_UNSUPPORTED, "too many programs for one launch");
     // ---- shares
-    int64_t length = W * page_size;
+    int64_t length = (int64_t)a.width * page_size;
     if (max_length) length = std::min(length, max_length);
     if (window) length = std::min(length, window + most);
     const int64_t block = rows == kManyRows ? many_keys(built) : few_trip(kind, built);

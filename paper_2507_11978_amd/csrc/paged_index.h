@@ -23,15 +23,25 @@ NT_HD uint32_t divide(uint32_t n, const Divider &d) { return (uint32_t)(((uint64
 
 NT_HD int32_t clamp_i32(int32_t v, int32_t lo, int32_t hi) { return v < lo ? lo : v > hi ? hi : v; }
 
+// Positions end here: the ends of blocks, and keys that are looked up ahead of their block, are below 2^31 too.
+constexpr int32_t kMostKeys = 0x7fffffff - 4095;
+
+// Entries of a table row, `width` long, that name positions below kMostKeys
+inline int32_t entries_in_reach(int64_t width, uint32_t page_size)
+{
+    const int64_t most = kMostKeys / page_size;
+    return (int32_t)(width < most ? width : most);
+}
+
 // A sequence: its first row of the queries, its new tokens, its tokens in the cache (with the new ones)
 struct Sequence {
     int32_t first, count, length;
 };
-// ... number b.  Whatever the arrays hold, [first, first + count) lies inside [0, T].
+// ... number b.  Whatever the arrays hold, [first, first + count) lies inside [0, T], and the length is at most what no table reaches.
 NT_HD Sequence sequence_at(const int32_t *starts, const int32_t *lengths, int b, int32_t T)
 {
     const int32_t s0 = clamp_i32(starts[b], 0, T), s1 = clamp_i32(starts[b + 1], s0, T), n = lengths[b];
-    return Sequence{s0, s1 - s0, n > 0 ? n : 0};
+    return Sequence{s0, s1 - s0, clamp_i32(n, 0, kMostKeys + 1)};
 }
 
 // The keys that token i of the sequence sees, [lo, hi) (none if hi <= lo).  Its position is length - count + i; negative where the length is too small
@@ -46,10 +56,14 @@ NT_HD KeyRange keys_seen(const Sequence &q, int32_t i, int32_t causal, int32_t w
 }
 
 // The keys [lo, hi) inside the sequence that some of tokens i0 .. i1 sees, and of them share number `split` of `splits`: share_keys each (the last: what is
-// left), from the first key on, rounded down to a multiple of `block`.
-NT_HD KeyRange key_range(const Sequence &q, int32_t i0, int32_t i1, int32_t causal, int32_t window, int split, int splits, int32_t share_keys, int32_t block)
+// left), from the first key on, rounded down to a multiple of `block`.  Of the positions from `capacity` on, which the table has no entry for, a token that sees any
+// needs one to show it: the first that it sees.  The range ends behind those, however long the sequence is said to be.
+NT_HD KeyRange key_range(const Sequence &q, int32_t i0, int32_t i1, int32_t causal, int32_t window, int split, int splits, int32_t share_keys, int32_t block,
+                         int32_t capacity = kMostKeys)
 {
     int32_t lo = keys_seen(q, i0, causal, window).lo, hi = keys_seen(q, i1, causal, window).hi;
+    const int32_t last = keys_seen(q, i1, causal, window).lo, enough = last > capacity ? last : capacity;
+    hi = hi > enough ? enough + 1 : hi;
     lo = lo > 0 ? lo : 0;
     hi = hi > 0 ? hi : 0;
     if (splits > 1) {

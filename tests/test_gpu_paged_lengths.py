@@ -1,0 +1,32 @@
+"""Lengths far beyond what the page table has room for: tokens that see such a position get NaN, soon, and nothing else changes."""
+import pytest
+import torch
+
+import paper_2507_11978_amd as nt
+from test_gpu_paged import KINDS, Batch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dt,kind", KINDS)
+@pytest.mark.parametrize("seqs,hints", [([(1, 40), (2, 33), (1, 64)], (2, 64)), ([(70, 150), (3, 40), (130, 131)], (0, 0)), ([(1, 3000), (1, 2900)], (1, 3000)), ([(40, 2000), (9, 1800)], (40, 2000))])
+@pytest.mark.parametrize("window", [0, 5, 100])
+def test_lengths_that_no_cache_has(dt, kind, seqs, hints, window):
+    b = Batch(seqs, 4, 2, 64, 16, dt, kind)
+    more = dict(window=window, max_queries=hints[0], max_length=hints[1])
+    want = b.run(**more).clone()
+    torch.cuda.synchronize()
+    shares = nt.last_paged_plan().shares
+    for length in (2 ** 31 - 1, 2 ** 31 - 64, 2 ** 31 - 4096, 2 ** 31 - 4097, 0x7f7f7f7f, 10 ** 9):
+        b.lengths[0] = length
+        got = b.run(**more)
+        torch.cuda.synchronize()
+        assert torch.isnan(got[:b.starts[1]]).all() and torch.equal(got[b.starts[1]:], want[b.starts[1]:])
+    assert shares > 1 or hints[1] < 1000 or window or (hints[0] == 1 and kind != "same")          # (375 KB of codes to a head are not shared)
+    # an end just behind the table's: the tokens whose window lies before it are what they are
+    reach = 16 * b.table.shape[1]
+    b.lengths[0] = reach + 1
+    got = b.run(**more)
+    assert torch.isnan(got[b.starts[1] - 1]).all()
+    assert torch.equal(got[b.starts[1]:], want[b.starts[1]:])
+    assert torch.isnan(b.run(**more, causal=False)[:b.starts[1]]).all()
