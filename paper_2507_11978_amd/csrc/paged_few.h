@@ -79,9 +79,8 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
 #pragma unroll
         for (int u = 0; u < NG; ++u) {
             const uint32_t index = divide((uint32_t)t * TRIP + 16 * u + (UNIFORM ? 0 : c16), g.page);
-            // (past the row's end: its last entry is read, and not used; a table without entries is replaced by the launcher)
-            const uint32_t inside = index < (uint32_t)g.width ? index : g.width > 0 ? g.width - 1 : 0;
-            id[u] = UNIFORM ? ((ScalarTable)pages)[inside] : pages[inside];
+            const uint32_t entry = entry_read(index, g.width);
+            id[u] = UNIFORM ? ((ScalarTable)pages)[entry] : pages[entry];
         }
     };
     auto locate = [&](int t, uint32_t (&has)[NG]) {
@@ -89,7 +88,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
 #pragma unroll
         for (int u = 0; u < NG; ++u) {
             const uint32_t key = (uint32_t)t * TRIP + 16 * u + (UNIFORM ? 0 : c16), index = divide(key, g.page), at = key - index * g.page.d;
-            const bool ok = index < (uint32_t)g.width && (uint32_t)id[u] < (uint32_t)g.pages;
+            const bool ok = names_page(index, id[u], g.width, g.pages);
             page[u] = ok ? id[u] : 0;
             has[u] = UNIFORM ? (ok ? 0xffffu : 0u) : (uint32_t)__ballot(ok) & 0xffffu;
             k_at[u] = (times(page[u], g.k_sp) + times(at, g.k_ss)) * ES;

@@ -74,12 +74,18 @@ NT_HD KeyRange key_range(const Sequence &q, int32_t i0, int32_t i1, int32_t caus
     return KeyRange{lo, hi < lo ? lo : hi};
 }
 
-// Entry `index` of a table row; -1: past its end, or no page of the cache
+// The page of a position, in two steps: its entry of the table row is on its way long before the page is needed.
+// Which entry is read for number `index`: past the row's end its last, which is not used then (of a row without entries the first: the launcher puts something
+// to read in its place)
+NT_HD uint32_t entry_read(uint32_t index, int32_t width) { return index < (uint32_t)width ? index : width > 0 ? (uint32_t)width - 1 : 0; }
+// Whether `id`, read so, names a page of the cache for entry `index`
+NT_HD bool names_page(uint32_t index, int32_t id, int32_t width, int32_t pages) { return index < (uint32_t)width && (uint32_t)id < (uint32_t)pages; }
+// Both steps: the page, -1 if none is named (the kernels take them apart; host checks call this)
 NT_HD int32_t page_at(const int32_t *row, uint32_t index, int32_t width, int32_t pages)
 {
-    if (index >= (uint32_t)width) return -1;
-    const int32_t id = row[index];
-    return (uint32_t)id < (uint32_t)pages ? id : -1;
+    if (width <= 0) return -1;
+    const int32_t id = row[entry_read(index, width)];
+    return names_page(index, id, width, pages) ? id : -1;
 }
 
 // Tiles of `rows` (token, query head) rows, `group` heads to a token: sequence b's are numbered from here on.  Rounding the rows before it down and adding b

@@ -114,12 +114,11 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
     const bool of_v = (lane / PER) & 1;
     const int64_t lane_sp = of_v ? g.v_sp : g.k_sp, lane_ss = of_v ? g.v_ss : g.k_ss;
     const char *const lane_base = of_v ? Vh : Kh;
-    auto entry = [&](uint32_t index) { return index < (uint32_t)g.width ? index : g.width > 0 ? g.width - 1 : 0; };      // (see paged_few.h)
     auto row_of = [&](int kb, int u) { return (uint32_t)(kb * KB + u * RSTEP + (FAST ? wave * (RSTEP / 4) : row0)); };
     auto find = [&](int kb) {
 #pragma unroll
-        for (int u = 0; u < (FAST ? 1 : PER); ++u) id[u] = pages[entry(divide(row_of(kb, FAST ? lane % PER : u), g.page))];
-        if constexpr (KIND != CACHE_SAME) sid = pages[entry(divide((uint32_t)(kb * KB + tid % KB), g.page))];
+        for (int u = 0; u < (FAST ? 1 : PER); ++u) id[u] = pages[entry_read(divide(row_of(kb, FAST ? lane % PER : u), g.page), g.width)];
+        if constexpr (KIND != CACHE_SAME) sid = pages[entry_read(divide((uint32_t)(kb * KB + tid % KB), g.page), g.width)];
     };
     // byte offsets within the wavefront's rows (FAST).  Straight into LDS: a lane's 16 bytes land at lane * 16, so it fetches the piece that belongs there; of
     // rows that lie 8 apart (head size 256) the order of the pieces differs in its last bit.
@@ -137,7 +136,7 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
 #pragma unroll
         for (int u = 0; u < (FAST ? 1 : PER); ++u) {
             const uint32_t key = row_of(kb, FAST ? lane % PER : u), index = divide(key, g.page), at = key - index * g.page.d;
-            const bool ok = index < (uint32_t)g.width && (uint32_t)id[u] < (uint32_t)g.pages;
+            const bool ok = names_page(index, id[u], g.width, g.pages);
             const uint32_t page = ok ? id[u] : 0;
             if constexpr (FAST) {
                 named = (uint32_t)__ballot(ok) & ((1u << PER) - 1);
@@ -186,7 +185,7 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
         }
         if constexpr (KIND != CACHE_SAME) {
             const uint32_t key = kb * KB + tid % KB, index = divide(key, g.page), at = key - index * g.page.d;
-            const uint32_t page = index < (uint32_t)g.width && (uint32_t)sid < (uint32_t)g.pages ? sid : 0;
+            const uint32_t page = names_page(index, sid, g.width, g.pages) ? sid : 0;
             sc = tid < KB ? g.KS[times(page, g.ks_sp) + times(at, g.ks_ss) + (int64_t)h * g.ks_sh] : g.VS[times(page, g.vs_sp) + times(at, g.vs_ss) + (int64_t)h * g.vs_sh];
         }
     };
