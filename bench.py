@@ -26,7 +26,7 @@ MFMA_PEAK_TFLOPS = 2500.0          # MI355X dense fp16/bf16 matrix peak (publish
 HBM_PEAK_GBS = 8000.0
 
 # HBM bytes per launch of the dominant kernel, measured with rocprofv3 --pmc (FETCH_SIZE and WRITE_SIZE runs, scaled by a copy
-# kernel of known size): profiles/traffic.json holds, per workload, the bytes and the library version they were measured on; a
+# kernel of known size): profiles/traffic.json holds, per workload, the bytes, the kernel and the library version they were measured on; a
 # figure measured on another version of the kernels is not reported.
 def measured_traffic(workload, version):
     try:
