@@ -253,17 +253,15 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) clear = clear && row_lo[mb] <= base && base + TRIP <= row_hi[mb];
             clear = __all(clear);
-            bool careful = false;
+            bool careful = false;                                          // (codes: some row does not see a NaN)
             if (all != 0xffffu || !clear) {                                // wavefront-uniform
-                bool odd = false;                                          // (an infinity or NaN among this lane's values)
+                bool odd = false;
 #pragma unroll
                 for (int u = 0; u < NG; ++u)
 #pragma unroll
                     for (int n = 0; n < NV; ++n) {
                         vr[u][n] = (good[u] >> c16) & 1 ? vr[u][n] : u32x4{0, 0, 0, 0};
-                        if constexpr (KIND == CACHE_SAME)
-                            odd = odd | any_not_finite<BF16>(vr[u][n]);
-                        else if constexpr (KIND == CACHE_E4M3)             // (0x7f, the type's one NaN)
+                        if constexpr (KIND == CACHE_E4M3)                  // (0x7f, the type's one NaN)
 #pragma unroll
                             for (int i = 0; i < 4; ++i) {
                                 const uint32_t x = vr[u][n][i] & 0x7f7f7f7fu;
@@ -349,6 +347,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
                 wavefront_fence();                                         // (the reads of the tile before are done)
+                ushort2v top{0, 0};                                        // largest magnitude among this lane's values, as integers: infinities and NaN above all numbers
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
 #pragma unroll
@@ -357,6 +356,8 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
                         const u32x4 x = vr[2 * i + u][n];
                         if constexpr (KIND == CACHE_SAME) {
                             lds_write16(vt, lds_at<SIZE>(row, 4 * n + g4), x);
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) top = __builtin_elementwise_max(top, __builtin_bit_cast(ushort2v, x[w] & 0x7fff7fffu));
                         } else {
                             lds_write16(vt, lds_at<SIZE>(row, 8 * n + 2 * g4), widen8<VB, KIND>(u32x2{x[0], x[1]}));
                             lds_write16(vt, lds_at<SIZE>(row, 8 * n + 2 * g4 + 1), widen8<VB, KIND>(u32x2{x[2], x[3]}));
@@ -365,8 +366,10 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
                     load_v(2 * i + u, more);
                 }
                 wavefront_fence();
-                if (careful) {
-                    // infinities and NaN of keys that only some rows see: added to those rows alone, and taken out of the tile
+                constexpr uint16_t ABOVE = BF16 ? 0x7f80 : 0x7c00;
+                if (KIND == CACHE_SAME ? __any(top[0] >= ABOVE || top[1] >= ABOVE) : careful) {
+                    // infinities and NaN: added to the rows that see their keys alone, and taken out of the tile (a weight of 0 does not silence them, and with one in
+                    // two parts an infinity would become infinity less infinity)
                     const int lane_here = here(lane), c = lane_here & 15, q = lane_here >> 4;
 #pragma unroll 1
                     for (int j = 0; j < 32; ++j)
