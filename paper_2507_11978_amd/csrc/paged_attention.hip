@@ -156,7 +156,7 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     a.T = (int32_t)T; a.B = (int32_t)B; a.Hq = (int32_t)Hq; a.Hkv = (int32_t)Hkv; a.G = (int32_t)(Hq / Hkv); a.D = (int32_t)D;
     a.width = entries_in_reach(W, (uint32_t)page_size); a.pages = (int32_t)pages;
     a.causal = causal ? 1 : 0;
-    a.window = (int32_t)std::min<int64_t>(window, 1 << 30);
+    a.window = (int32_t)std::min<int64_t>(window, 0x7fffffff);              // (longer than any sequence)
     const int64_t es = kind == CACHE_SAME ? 2 : 1, most_bytes = (1LL << 31) - 4096;
     a.near = a.k_ss >= 0 && a.k_ss < most_bytes / (16 * es) && a.v_ss >= 0 && a.v_ss < most_bytes / (16 * es);
     a.uniform = a.near && page_size % 16 == 0;

@@ -52,7 +52,7 @@ struct KeyRange {
 NT_HD KeyRange keys_seen(const Sequence &q, int32_t i, int32_t causal, int32_t window)
 {
     const int32_t pos = q.length - q.count + i;
-    return KeyRange{window ? pos - window + 1 : 0, causal && pos + 1 < q.length ? pos + 1 : q.length};
+    return KeyRange{window && pos >= window ? pos - window + 1 : 0, causal && pos + 1 < q.length ? pos + 1 : q.length};
 }
 
 // The keys [lo, hi) inside the sequence that some of tokens i0 .. i1 sees, and of them share number `split` of `splits`: share_keys each (the last: what is

@@ -30,3 +30,20 @@ def test_lengths_that_no_cache_has(dt, kind, seqs, hints, window):
     assert torch.isnan(got[b.starts[1] - 1]).all()
     assert torch.equal(got[b.starts[1]:], want[b.starts[1]:])
     assert torch.isnan(b.run(**more, causal=False)[:b.starts[1]]).all()
+
+
+@pytest.mark.parametrize("window,sees", [(0, True), (2 ** 30, False), (2 ** 30 + 2 ** 19, False), (2 ** 30 + 2 ** 20, True), (2 ** 31 - 1, True), (2 ** 40, True)])
+def test_windows_longer_than_two_to_the_30(window, sees):
+    """A table that names one page again and again, and another at its beginning, whose keys outweigh all the rest."""
+    size, page, length = 8, 4096, 2 ** 30 + 2 ** 20
+    k, v = torch.zeros(2, page, 1, size, dtype=torch.int8, device="cuda"), torch.ones(2, page, 1, size, dtype=torch.int8, device="cuda")
+    k[1, :, :, 0], v[1] = 100, 7
+    scale = torch.ones(2, page, 1, device="cuda")
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    table = torch.zeros(1, length // page, dtype=torch.int32, device="cuda")
+    table[0, 0] = 1
+    q = torch.zeros(1, 1, size, dtype=torch.float16, device="cuda")
+    q[..., 0] = 1.0
+    out = nt.sdpa_paged(q, k, v, table, i32([0, 1]), i32([length]), torch.empty_like(q), scale, scale, scale=0.5, window=window, max_queries=1, max_length=length)
+    torch.cuda.synchronize()
+    assert torch.equal(out, torch.full_like(q, 7.0 if sees else 1.0)), out

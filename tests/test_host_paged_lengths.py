@@ -67,6 +67,15 @@ int main()
             CHECK(index == key / page && (index < (uint32_t)width) == (key < capacity));
         }
     }
+    // windows of any length
+    for (int i = 0; i < 200000; ++i) {
+        const int32_t count = (int32_t)in(1, 1 << 30), length = (int32_t)in(0, kMostKeys + 1), window = (int32_t)(INT32_MAX - (in(0, 1) ? in(0, 1 << 20) : in(0, INT32_MAX - 1)));
+        const Sequence q{0, count, length};
+        const int32_t t = (int32_t)in(0, count - 1);
+        const KeyRange k = keys_seen(q, t, 1, window);
+        const int64_t pos = (int64_t)length - count + t, lo = pos - window + 1;
+        CHECK(k.hi == pos + 1 && (int64_t)(k.lo > 0 ? k.lo : 0) == (lo > 0 ? lo : 0));
+    }
     puts("good");
 }
 """
