@@ -365,15 +365,16 @@ nt_status nt_cache_read(const nt_paged_cache *cache, void *k, const nt_tensor_de
  * decreasing) and lengths: device int32 arrays.
  *   out[t,h,:] = sum_j softmax_j(scale <q[t,h,:], K_j>) V_j  over the positions 0 <= j < lengths[b] that the token sees:
  *   j <= p if `causal`, and j > p - window if window > 0.
- * What a token does not see has no part in its result, whatever it holds.  A token that sees nothing (a length below the new tokens' count, or 0), or
- * nothing with a score above -inf, gets zeros.  A token that sees a position whose page the table does not name (an entry outside the
- * cache, such as -1, or a position past the table's last entry, or past 2^31 - 4097, which no table reaches) gets NaN.  Rows of q that belong to no sequence are passed over.  scale = 0
- * stands for 1 / sqrt(head_size).  out must not alias an input.
+ * What a token does not see has no part in its result, whatever it holds; an infinity among the values that it sees makes that element an
+ * infinity or NaN.  A token that sees nothing (a length below the new tokens' count, or 0), or nothing with a score above -inf, gets zeros.
+ * A token that sees a position whose page the table does not name (an entry outside the cache, such as -1, or a position past the table's last
+ * entry, or past 2^31 - 4097, which no table reaches) gets NaN.  Rows of q that belong to no sequence are passed over.  scale = 0 stands for
+ * 1 / sqrt(head_size).  out must not alias an input.
  * Scores, weights' sums and accumulators are fp32.  Over an 8-bit cache K's scale multiplies the score and V's the weight, in fp32.  What multiplies V then
  * is the weight as the sum of two numbers of `dtype` (bf16 over codes), off by 2^-17 of it at most (fp16: 2^-23, or 2^-25 of a weight of 1), where a
  * program has 16 or 32 rows, and over codes with NT_F16; otherwise, in whole chunks, as one number, off by half a step of the type (bf16 2^-8, fp16 2^-11).
  * max_queries, max_length: the most new tokens and the greatest length of a sequence, if the host knows them (0: it does not); they choose the
- * kernel and how the keys are shared out, so a bound that is too low costs time, not results.
+ * kernel and how the keys are shared out, so a bound that is too low costs time and is not an error.
  * Memory: the keys of long sequences are shared out over programs where there are few of them; the shares pass through the library's
  * workspace under the rules given at nt_conv2d_implicit, and are added in a fixed order.
  */

@@ -180,11 +180,11 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     const int64_t block = rows == kManyRows ? many_keys(built) : few_trip(kind, built);
     int64_t splits;
     if (rows == kManyRows) {
-        // Two programs for a unit, of 192 keys each and more (us, graph replays, 32/8 heads x 128 bf16: 64 queries x 600 keys 22 unshared, 15.1 in 3 shares,
+        // Below 256 programs as many shares as make two for a unit at most, of 192 keys each and more; from 256 on, one program to a unit and more, none (us, graph replays, 32/8 heads x 128 bf16: 64 queries x 600 keys 22 unshared, 15.1 in 3 shares,
         // 1000 30 / 17.2 in 4, 20000 526 / 49.5 in 32; 200 x 4000 109 / 38.4 in 8, 60.3 in 16; 7 x 200 in windows of 512 29.6 / 29.1 in 3).
         splits = std::min(base >= 256 ? 1 : 512 / base, length / 192);
     } else {
-        // As many programs as units, of 48 KB of K and V and more each (us, graph replays: 1 x 8 heads x 128 bf16, 500 keys 12.0 unshared, 9.5 in 6 shares, 2000 32.3 / 10.7
+        // As many programs as units at most, of 48 KB of K and V and more each (us, graph replays: 1 x 8 heads x 128 bf16, 500 keys 12.0 unshared, 9.5 in 6 shares, 2000 32.3 / 10.7
         // in 21, 32000 434 / 31.0 in 32, 31.2 in 63; 48 heads x 64 f16, 900 12.2 / 10.6 in 4, 12.3 in 3, 8000 60.0 / 24.5 in 4, 28.3 in 8; 300 9.1 / 9.7 in 3).
         const int64_t key_bytes = 2 * D * es, total = length * key_bytes;
         // Below 384 KB to a sequence's head not at all: the second launch and the workspace's event are 4 us of the host's time (48 x 900, called: 12.5 us, 13.2).

@@ -15,8 +15,9 @@
 // 131072 e4m3 128 and 129), but for two sets of 16 rows over codes (8 x 8 queries x 4000 keys x 32/8 heads x 128 e4m3 30.7 us, 32.8).  Rounded once they would be off
 // by as much as the rounded result.
 //
-// Bound by reading K and V: 64 sequences of 17 to 4096 tokens, 32/8 heads x 128 bf16 134 us = 4.15 TB/s (a large copy reaches 4.84), 2 of 131072 in e4m3 128 us =
-// 4.3 TB/s, 32 of 2047 with 48 heads x 64 in int8 62.5 us = 4.6 TB/s; one of 900 12.5 us, most of it the host's call and one wavefront's chain of loads.
+// Bound by reading K and V: 64 sequences of 17 to 4096 tokens, 32/8 heads x 128 bf16 134 us = 4.15 TB/s (a large copy reaches 4.84), 2 of 131072 in e4m3 129 us =
+// 4.3 TB/s, 32 of 2047 with 48 heads x 64 in int8 63.6 us = 4.5 TB/s; the matrix pipe is busy for 4 to 8 % of the cycles, 1.03 of their bytes are read.  One of 900
+// 12.5 us, most of it the host's call and one wavefront's chain of loads.
 #pragma once
 #include "paged.h"
 

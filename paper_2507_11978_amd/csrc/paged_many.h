@@ -15,11 +15,13 @@
 // them, so that these lie on one page): the table is read and the addresses are made by one lane for all.  A 16-bit cache then travels straight into
 // LDS, one block ahead, codes through registers, 16 at a time.  Other caches: 8 elements to a lane through registers, every lane with an address of its own.
 //
-// Measured: 2048 queries of 32/8 heads x 128 bf16 over 18500 keys 628 to 645 us = 0.91 to 0.93 PFLOP/s (a large matrix product reaches 1.18), 1024 queries x 8000 214, over
-// e4m3 315, int8 328 (each lane widens 64 elements of a block and scales 64 scores and weights).  A block of 64 keys is 32 matrix instructions of 32 cycles
-// and 4 of 16 to a wavefront beside 32 exponentials, the multiplications and packs that feed them; the matrix pipe is busy for 36 % of the cycles, LDS has
-// no conflicts.  Two wavefronts to a SIMD (128; three at 64) are what the registers allow, and where both weigh their blocks the pipe waits.  Tried: the next block's products between this block's exponentials (K two blocks ahead, two
-// sets of scores): 629 us with all 256 registers, but 7.5 % slower at head size 64 and half again as long where registers ran out; blocks of 32 keys: 775.
+// Measured: 2048 queries of 32/8 heads x 128 bf16 over 18500 keys 620 to 650 us = 0.90 to 0.94 PFLOP/s (a large matrix product reaches 1.18), 1024 queries x 8000 211, over
+// e4m3 290 to 297, int8 304 to 310 (each lane widens 64 elements of a block and scales 64 scores and weights), fp16 over them 365 and 376.  A block of 64 keys is
+// 32 matrix instructions of 32 cycles and 4 of 16 to a wavefront beside 32 exponentials, the multiplications and packs that feed them; the matrix pipe is busy for
+// 44 % of the cycles, LDS has no conflicts.  Two wavefronts to a SIMD (128; three at 64) are what the registers allow, and where both weigh their blocks the pipe
+// waits.  Tried: the next block's products between this block's exponentials (K two blocks ahead, two sets of scores): 629 us with all 256 registers, but 7.5 %
+// slower at head size 64 and half again as long where registers ran out; blocks of 32 keys: 775.  Hidden keys of codes told by their weight in every block, not
+// by position in those that have any: 8 % longer.
 #pragma once
 #include "paged.h"
 
@@ -35,7 +37,7 @@ constexpr size_t many_block(int size) { return (size_t)many_keys(size) * size * 
 constexpr size_t many_lds(int size) { return 4 * many_block(size) + 2 * 2 * many_keys(size) * 4 + 16; }
 
 // Wavefronts per SIMD that the registers are shared out for.  Codes at head size 64 do better with more registers (2 x 1024 queries x 8000 keys x 16 heads f16 over int8
-// 396 us with three, 349; bf16, half of that, 119, 113), 16-bit caches use 168.
+// 396 us with three, 349 when that was measured, 316 since; bf16, half of that, 119, 113), 16-bit caches use 168.
 constexpr int many_resident(int kind, int size) { return size == 256 ? 1 : size == 128 || kind != CACHE_SAME ? 2 : 3; }
 
 // FULL: rows of SIZE elements (the switched-off lanes of others cost 5 % where none is: 1024 queries x 8000 keys x 32/8 heads x 128 bf16 217 us, 228)

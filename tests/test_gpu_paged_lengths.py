@@ -47,3 +47,23 @@ def test_windows_longer_than_two_to_the_30(window, sees):
     out = nt.sdpa_paged(q, k, v, table, i32([0, 1]), i32([length]), torch.empty_like(q), scale, scale, scale=0.5, window=window, max_queries=1, max_length=length)
     torch.cuda.synchronize()
     assert torch.equal(out, torch.full_like(q, 7.0 if sees else 1.0)), out
+
+
+def test_shares_that_do_not_fit_the_workspace():
+    """64 sequences of 131072: their shares' partial results would take more than the library's 256 MB.  Tables that name one page again and again: the result is that
+    over the page."""
+    size, page, heads, group, count, length = 128, 16, 8, 4, 64, 131072
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k, v = (torch.randn(1, page, heads, size, generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn(count, heads * group, size, generator=g, device="cuda").bfloat16()
+    i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    lengths = [length - 16 * 1000 * (b % 5) for b in range(count)]
+    out = nt.sdpa_paged(q, k, v, torch.zeros(count, length // page, dtype=torch.int32, device="cuda"), i32(list(range(count + 1))), i32(lengths), torch.empty_like(q),
+                        max_queries=1, max_length=length)
+    torch.cuda.synchronize()
+    K, V = (t[0].double().cpu().permute(1, 0, 2).repeat_interleave(group, 0) for t in (k, v))           # [query heads, keys, size]
+    p = torch.softmax((q.double().cpu()[:, :, None] * K).sum(-1) / size ** 0.5, -1)
+    want, A = ((p[..., None] * x).sum(2) for x in (V, V.abs()))
+    # the result's rounding; sums of 131072 fp32 numbers, and scores' (size + 8 roundings of at most 4 sqrt(size) (1 + largest score))
+    tol = 2.0 ** -8 * want.abs() + A * 2.0 ** -24 * (length + 2 * (size + 8) * 4 * size ** 0.5 * 6)
+    assert ((out.double().cpu() - want).abs() <= tol).all()
