@@ -382,7 +382,72 @@ nt_status nt_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_paged_
                         const int32_t *starts, const int32_t *lengths, void *out, const nt_tensor_desc *dout,
                         float scale, int32_t causal, int64_t window, int64_t max_queries, int64_t max_length, nt_dtype dtype, void *hip_stream);
 
-/* How the calling thread's last nt_sdpa_paged call was laid out; zeros if nothing was launched.  For tests and diagnostics. */
+/* ---------------------------------------------------------------- drafted tokens over a paged cache (device)
+ *
+ * A step of a program that drafts: nt_cache_fit gives the new tokens pages, slots and positions, nt_tree_masks tells who sees whom, nt_cache_write and
+ * nt_sdpa_paged_tree run over all of them in every layer, nt_verify_tree says which stand and what follows them, nt_cache_compact moves what stands to where
+ * it belongs.  Nothing of it needs the host to know a length.
+ * The new tokens lie one sequence behind the other: sequence b has tokens starts[b] .. starts[b + 1] - 1 (device int32, sequences + 1 entries, not decreasing).  They are
+ * a tree: parents[t] is the number of token t's parent among its sequence's new tokens, from 0, less than its own; anything else stands for none.
+ *
+ * nt_cache_fit: the pages of a cache handed out on the device.  All arrays are device arrays, int32 but for slots.  Sequence b has lengths[b] tokens and gets
+ * counts[b] more (negative ones count as 0); it holds the pages table[b][0] .. table[b][held[b] - 1].  free_pages[0] .. free_pages[*free_count - 1] is a stack of the pages that
+ * no one holds, with room for `capacity`, all the pages there are.  Afterwards
+ *   new_lengths[b] = lengths[b] + counts[b], and it holds ceil(new_lengths[b] / page_size) pages (as many as a row of the table has entries, at most): those beyond that
+ *                    have gone back onto the stack, from the last sequence's last to the first's first, missing ones have been taken off it, from the first
+ *                    sequence's first to the last's last.  held and *free_count are brought up to date, entries of the table beyond held are as they were.
+ *   starts         = the sums of counts, sequences + 1 of them;
+ *   slots[t], positions[t] (int64, int32; t < tokens): of new token t, its slot for nt_cache_write and its position in its sequence.  Behind the last new token: -1 and 0.
+ * A sequence that is over has lengths[b] = counts[b] = 0 and gives everything back.  Where the stack runs out, sequences go without, the last first: the entries they lack
+ * are -1, held does not count them, their tokens' slots are -1, and *free_count is less than 0 by the number of missing pages (and counts as 0 in the next call).  Slots past the
+ * table's row are -1 too.  new_lengths may be lengths itself.  No other two arrays may overlap.
+ */
+nt_status nt_cache_fit(const int32_t *lengths, const int32_t *counts, int64_t sequences, int64_t page_size, int32_t *table, const nt_tensor_desc *d_table,
+                       int32_t *held, int32_t *free_pages, int64_t capacity, int32_t *free_count, int32_t *starts, int32_t *new_lengths,
+                       int64_t *slots, int32_t *positions, int64_t tokens, void *hip_stream);
+
+/* nt_tree_masks: who sees whom in a tree.  masks: device uint64 [tokens, words] (any stride along tokens, unit stride along words): bit j % 64 of word j / 64 of token t's row is
+ * set where new token j of t's sequence is t or an ancestor of it (window > 0: at most window - 1 steps up).  Bits that 64 * words do not hold are left out.
+ * depths[t] (device int32): how many ancestors t has.  positions[t] = lengths[b] - n + depths[t], n the sequence's new tokens, lengths with them (both or
+ * neither may be NULL).  Rows of no sequence are left as they are. */
+nt_status nt_tree_masks(const int32_t *parents, const int32_t *starts, int64_t sequences, uint64_t *masks, const nt_tensor_desc *d_masks, int32_t *depths,
+                        const int32_t *lengths, int32_t *positions, int64_t window, void *hip_stream);
+
+/* nt_sdpa_paged_tree: nt_sdpa_paged for trees.  New token i of n of sequence b sees the past, positions 0 <= j < lengths[b] - n, and of the new tokens, at positions
+ * lengths[b] - n + k, those whose bit k is set in its row of masks (as nt_tree_masks makes them; any bits will do, a token need not see itself; bits of
+ * numbers from n on mean nothing).  window > 0: of the past the positions j > lengths[b] - n + depths[t] - window (depths[t] is taken as 0 to n - 1; needed with a window only).
+ * Everything else, a token that sees nothing or a position without a page, precision, memory, and max_queries and max_length, as nt_sdpa_paged. */
+nt_status nt_sdpa_paged_tree(const void *q, const nt_tensor_desc *dq, const nt_paged_cache *cache, const int32_t *table, const nt_tensor_desc *d_table,
+                             const int32_t *starts, const int32_t *lengths, const uint64_t *masks, const nt_tensor_desc *d_masks, const int32_t *depths,
+                             void *out, const nt_tensor_desc *dout, float scale, int64_t window, int64_t max_queries, int64_t max_length, nt_dtype dtype, void *hip_stream);
+
+/* nt_verify_tree: which drafted tokens stand, and the token behind them.  A sequence's new token 0 is the root, a token that stands already; the others are drafts.
+ * target [tokens, vocabulary]: row t is the target's distribution behind token t.  draft: row t is the one that t's children were drawn from, or NULL:
+ * the drafts are taken as certain.  Both have elements of `dtype` (NT_F32, NT_F16, NT_BF16), any stride along tokens, unit stride along the vocabulary; what is not a positive
+ * finite number counts as 0.  ids (device int64): the tokens; uniform[t] and last_uniform[b] (device float): random numbers in [0, 1).
+ *   At a node, from the root on:  w = its target row, m = 1;  for each child in the order of their numbers, x its token, u its random number, q the node's draft row (1 without):
+ *     it stands if u q(x) m < w(x), and is the next node;  if not, w = max(w / m - q, 0) and m = the sum of w (0 everywhere where m was 0);  without q:
+ *     m = max(m - w(x), 0) and w(x) = 0.
+ *   Where no child stands, or the path is full, the next token is the first t with w(0) + .. + w(t) > last_uniform[b] * (the sum of w).  If w is 0 everywhere it is drawn
+ *   from the node's target row so, and is -1 if that is 0 everywhere too.
+ * Sums and comparisons are in 64 bits.  A draft outside the vocabulary is passed over, and so are a node's children behind its 64th.
+ * path (device int32 [sequences, room], unit stride along a row): the numbers of the tokens that stand, the root's 0 first, then -1;  accepted[b] (int32): how many,
+ * the root with them (no new tokens: 0, and next[b] = -1);  next[b] (int64): the next token;  new_lengths[b] = lengths[b] - n + accepted[b] (both or neither may be NULL; they may
+ * be one). */
+nt_status nt_verify_tree(const void *target, const nt_tensor_desc *d_target, const void *draft, const nt_tensor_desc *d_draft, const int64_t *ids,
+                         const int32_t *parents, const int32_t *starts, int64_t sequences, const float *uniform, const float *last_uniform,
+                         int32_t *path, const nt_tensor_desc *d_path, int32_t *accepted, int64_t *next, const int32_t *lengths, int32_t *new_lengths,
+                         nt_dtype dtype, void *hip_stream);
+
+/* nt_cache_compact: the tokens that stand, moved to the places behind the past.  Sequence b has lengths[b] tokens with its accepted[b] new ones that stand; with
+ * p = lengths[b] - accepted[b] the token at position p + path[b][k] goes to position p + k, for all k < accepted[b], as if all were read before any is written.
+ * lengths, path, accepted as nt_verify_tree leaves them (a row of path ascends; an entry that is not above its own place is not moved, nor is one whose
+ * positions have no page).  caches: a HOST array of n_caches caches (a program's layers) that share the page table, one type and one layout (else
+ * NT_ERR_SHAPE_MISMATCH).  Codes and scales are moved as they are. */
+nt_status nt_cache_compact(const nt_paged_cache *caches, int64_t n_caches, const int32_t *table, const nt_tensor_desc *d_table, const int32_t *lengths,
+                           const int32_t *path, const nt_tensor_desc *d_path, const int32_t *accepted, void *hip_stream);
+
+/* How the calling thread's last nt_sdpa_paged or nt_sdpa_paged_tree call was laid out; zeros if nothing was launched.  For tests and diagnostics. */
 typedef struct {
     int32_t rows;            /* (token, query head) rows per program: 16 or 32 (wavefronts share the keys), or 128 (they share the rows) */
     int32_t shares;          /* programs that a row's keys are shared out over */

@@ -140,6 +140,11 @@ def load():
     L.nt_cache_write.argtypes = [PC, P, D, P, D, P, i32, P]
     L.nt_cache_read.argtypes = [PC, P, D, P, D, P, i32, P]
     L.nt_sdpa_paged.argtypes = [P, D, PC, P, D, P, P, P, D, C.c_float, i32, i64, i64, i64, i32, P]
+    L.nt_sdpa_paged_tree.argtypes = [P, D, PC, P, D, P, P, P, D, P, P, D, C.c_float, i64, i64, i64, i32, P]
+    L.nt_cache_fit.argtypes = [P, P, i64, i64, P, D, P, P, i64, P, P, P, P, P, i64, P]
+    L.nt_tree_masks.argtypes = [P, P, i64, P, D, P, P, P, i64, P]
+    L.nt_verify_tree.argtypes = [P, D, P, D, P, P, P, i64, P, P, P, D, P, P, P, P, i32, P]
+    L.nt_cache_compact.argtypes = [PC, i64, P, D, P, P, D, P, P]
     L.nt_add.argtypes = [P, D, P, D, P, D, i32, i64, P]
     L.nt_silu.argtypes = [P, D, P, D, i32, i64, P]
     L.nt_softmax.argtypes = [P, D, P, D, i32, P]
@@ -150,7 +155,7 @@ def load():
     for name in ("nt_arrange_levels", "nt_arrange_tile", "nt_arrange_gemm", "nt_arrange_bmm", "nt_arrange_conv2d",
                  "nt_program_order", "nt_gemm", "nt_gemm_noalloc", "nt_addmm", "nt_addmm_act", "nt_bmm", "nt_conv2d_implicit", "nt_trace_tile", "nt_trace_loader_slice",
                  "nt_add", "nt_silu", "nt_softmax", "nt_rms_norm", "nt_matmul_views", "nt_sdpa", "nt_cache_write", "nt_cache_read",
-                 "nt_sdpa_paged", "nt_mfma_probe"):
+                 "nt_sdpa_paged", "nt_sdpa_paged_tree", "nt_cache_fit", "nt_tree_masks", "nt_verify_tree", "nt_cache_compact", "nt_mfma_probe"):
         getattr(L, name).restype = i32
     L.nt_last_kernel_path.restype = i32
     L.nt_last_k_split.restype = i32
@@ -195,7 +200,8 @@ def _load_calls():
         spec.loader.exec_module(module)
         module.bind(*(C.cast(getattr(lib, name), C.c_void_p).value
                       for name in ("nt_gemm", "nt_bmm", "nt_addmm", "nt_addmm_act", "nt_conv2d_implicit", "nt_sdpa", "nt_softmax", "nt_rms_norm", "nt_add", "nt_silu",
-                                   "nt_cache_write", "nt_cache_read", "nt_sdpa_paged")))
+                                   "nt_cache_write", "nt_cache_read", "nt_sdpa_paged", "nt_sdpa_paged_tree", "nt_cache_fit", "nt_tree_masks", "nt_verify_tree",
+                                   "nt_cache_compact")))
     except (ImportError, OSError) as e:                     # not built, or built for another torch
         module = _calls = _Declining()
         warnings.warn(f"{_CALLS_PATH} cannot be loaded ({e}): calls are marshalled through ctypes, some 2 us slower each; "
@@ -463,7 +469,7 @@ def last_sdpa_plan() -> SdpaPlan:
 
 
 def last_paged_plan() -> PagedPlan:
-    """How the calling thread's last sdpa_paged() was laid out."""
+    """How the calling thread's last sdpa_paged() or sdpa_paged_tree() was laid out."""
     plan = PagedPlan()
     _check(load().nt_last_paged_plan(C.byref(plan)))
     return plan
@@ -600,7 +606,11 @@ _cache_codes: dict = {}
 
 
 def _cache(k_cache, v_cache, k_scale, v_scale):
-    """The C description of a paged cache (a reference to it keeps it, and the descriptors it names, alive)."""
+    """A reference to the C description of a paged cache (it keeps that, and the descriptors it names, alive)."""
+    return C.byref(_cache_struct(k_cache, v_cache, k_scale, v_scale))
+
+
+def _cache_struct(k_cache, v_cache, k_scale, v_scale):
     import torch
     if not _cache_codes:
         _cache_codes.update({torch.float16: _DTYPES["f16"], torch.bfloat16: _DTYPES["bf16"], torch.float8_e4m3fn: 3, torch.int8: 4})
@@ -616,11 +626,11 @@ def _cache(k_cache, v_cache, k_scale, v_scale):
             raise ValueError("scales must be float32")
         descs += [make_desc(t.shape, t.stride()) for t in (k_scale, v_scale)]
         c.k_scale, c.v_scale, c.dks, c.dvs = k_scale.data_ptr(), v_scale.data_ptr(), C.pointer(descs[2]), C.pointer(descs[3])
-    return C.byref(c)
+    return c
 
 
 def _integers(t, dtype, name, count=None):
-    """A dense one-dimensional GPU tensor of integers, as an address."""
+    """A dense one-dimensional GPU tensor of numbers of this type, as an address."""
     _require_cuda(t)
     if t.dtype != dtype or t.dim() != 1 or not t.is_contiguous():
         raise ValueError(f"{name} must be a dense one-dimensional tensor of {dtype}")
@@ -692,6 +702,133 @@ def sdpa_paged(q, k_cache, v_cache, table, starts, lengths, out, k_scale=None, v
                                 out.data_ptr(), _ref(out), float(scale), int(bool(causal)), int(window), int(max_queries), int(max_length), code,
                                 _stream_ptr(stream)))
     return out
+
+
+def _rows(t, dtype, name):
+    """A two-dimensional GPU tensor of numbers of this type."""
+    _require_cuda(t)
+    if t.dtype != dtype or t.dim() != 2:
+        raise ValueError(f"{name} must be a two-dimensional tensor of {dtype}")
+    return t
+
+
+def sdpa_paged_tree(q, k_cache, v_cache, table, starts, lengths, masks, out, k_scale=None, v_scale=None, depths=None, scale=0.0, window=0, max_queries=0,
+                    max_length=0, stream=None):
+    """Attention of drafted trees' tokens over a paged cache: as sdpa_paged, but of the new tokens each sees those whose bit is set in its row of masks (int64
+    [tokens, words], see tree_masks), and of the past all, or the last ones within `window` of its depth (depths int32 [tokens], for a window).  See nt_sdpa_paged_tree."""
+    if _recorder is None:
+        st = (_calls or _load_calls()).sdpa_paged_tree(q, k_cache, v_cache, table, starts, lengths, masks, out, k_scale, v_scale, depths, scale, window, max_queries,
+                                                       max_length, stream)
+        if st is not None:
+            if st:
+                _check(st)
+            return out
+    import torch
+    _require_cuda(q, out)
+    if q.dtype != out.dtype:
+        raise ValueError("output must have the queries' dtype")
+    _rows(table, torch.int32, "table")
+    _rows(masks, torch.int64, "masks")
+    code = _code(q)
+    _check(load().nt_sdpa_paged_tree(q.data_ptr(), _ref(q), _cache(k_cache, v_cache, k_scale, v_scale), table.data_ptr(), _ref(table),
+                                     _integers(starts, torch.int32, "starts", table.shape[0] + 1), _integers(lengths, torch.int32, "lengths", table.shape[0]),
+                                     masks.data_ptr(), _ref(masks), None if depths is None else _integers(depths, torch.int32, "depths", q.shape[0]),
+                                     out.data_ptr(), _ref(out), float(scale), int(window), int(max_queries), int(max_length), code, _stream_ptr(stream)))
+    return out
+
+
+def cache_fit(lengths, counts, page_size, table, held, free_pages, free_count, starts, new_lengths, slots, positions, stream=None):
+    """Pages, slots and positions of a step's new tokens from the sequences' lengths, on the GPU: sequence b of lengths[b] tokens gets counts[b] more and the pages that it
+    needs with them, no more, from and to the stack free_pages (free_count [1] of them).  Brings table [sequences, entries], held [sequences], free_pages and
+    free_count up to date; gives starts [sequences + 1], new_lengths [sequences], slots (int64) and positions of the new tokens.  All else int32.  See nt_cache_fit."""
+    if _recorder is None:
+        st = (_calls or _load_calls()).cache_fit(lengths, counts, page_size, table, held, free_pages, free_count, starts, new_lengths, slots, positions, stream)
+        if st is not None:
+            if st:
+                _check(st)
+            return slots, positions
+    import torch
+    B, i32 = _rows(table, torch.int32, "table").shape[0], torch.int32
+    _check(load().nt_cache_fit(_integers(lengths, i32, "lengths", B), _integers(counts, i32, "counts", B), B, int(page_size), table.data_ptr(), _ref(table),
+                               _integers(held, i32, "held", B), _integers(free_pages, i32, "free_pages"), free_pages.numel(), _integers(free_count, i32, "free_count", 1),
+                               _integers(starts, i32, "starts", B + 1), _integers(new_lengths, i32, "new_lengths", B), _integers(slots, torch.int64, "slots"),
+                               _integers(positions, i32, "positions", slots.numel()), slots.numel(), _stream_ptr(stream)))
+    return slots, positions
+
+
+def tree_masks(parents, starts, masks, depths, lengths=None, positions=None, window=0, stream=None):
+    """Who sees whom in drafted trees: masks (int64 [tokens, words], a bit for each of a sequence's new tokens) of each token and its ancestors, depths [tokens], and, from
+    the lengths [sequences] with the new tokens, positions [tokens].  parents [tokens]: numbers within the sequence, -1: none.  See nt_tree_masks."""
+    if _recorder is None:
+        st = (_calls or _load_calls()).tree_masks(parents, starts, masks, depths, lengths, positions, window, stream)
+        if st is not None:
+            if st:
+                _check(st)
+            return masks, depths
+    import torch
+    T, i32 = _rows(masks, torch.int64, "masks").shape[0], torch.int32
+    if (lengths is None) != (positions is None):
+        raise ValueError("lengths and positions, or neither")
+    at = _integers(starts, i32, "starts")
+    B = starts.numel() - 1
+    if B < 0:
+        raise ValueError("starts must hold a number more than there are sequences")
+    _check(load().nt_tree_masks(_integers(parents, i32, "parents", T), at, B, masks.data_ptr(), _ref(masks), _integers(depths, i32, "depths", T),
+                                None if lengths is None else _integers(lengths, i32, "lengths", B), None if positions is None else _integers(positions, i32, "positions", T),
+                                int(window), _stream_ptr(stream)))
+    return masks, depths
+
+
+def verify_tree(target, draft, ids, parents, starts, uniform, last_uniform, path, accepted, next_ids, lengths=None, new_lengths=None, stream=None):
+    """Which drafted tokens stand, and the token behind them: target and draft (or None) [tokens, vocabulary] probabilities behind each token, ids (int64) and parents
+    of the tokens, random numbers uniform [tokens] and last_uniform [sequences] (float32).  Gives path [sequences, room], accepted [sequences], next_ids (int64
+    [sequences]) and, from lengths with all new tokens, new_lengths with those that stand.  See nt_verify_tree."""
+    if _recorder is None:
+        st = (_calls or _load_calls()).verify_tree(target, draft, ids, parents, starts, uniform, last_uniform, path, accepted, next_ids, lengths, new_lengths, stream)
+        if st is not None:
+            if st:
+                _check(st)
+            return accepted, next_ids
+    import torch
+    _require_cuda(target)
+    i32, f32 = torch.int32, torch.float32
+    if target.dim() != 2:
+        raise ValueError("target must be a two-dimensional tensor")
+    T, B = target.shape[0], _rows(path, i32, "path").shape[0]
+    if draft is not None:
+        _require_cuda(draft)
+        if draft.dtype != target.dtype:
+            raise ValueError("target and draft must have one type")
+    if (lengths is None) != (new_lengths is None):
+        raise ValueError("lengths and new lengths, or neither")
+    code = _code(target)
+    _check(load().nt_verify_tree(target.data_ptr(), _ref(target), None if draft is None else draft.data_ptr(), None if draft is None else _ref(draft),
+                                 _integers(ids, torch.int64, "ids", T), _integers(parents, i32, "parents", T), _integers(starts, i32, "starts", B + 1), B,
+                                 _integers(uniform, f32, "uniform", T), _integers(last_uniform, f32, "last_uniform", B), path.data_ptr(), _ref(path),
+                                 _integers(accepted, i32, "accepted", B), _integers(next_ids, torch.int64, "next_ids", B),
+                                 None if lengths is None else _integers(lengths, i32, "lengths", B),
+                                 None if new_lengths is None else _integers(new_lengths, i32, "new_lengths", B), code, _stream_ptr(stream)))
+    return accepted, next_ids
+
+
+def cache_compact(caches, table, lengths, path, accepted, stream=None):
+    """The tokens that stand moved to the places behind the past, in all of `caches` (a program's layers: (k, v) or (k, v, k_scale, v_scale) each, of one type and
+    layout) that the page table is of; lengths (with the tokens that stand), path and accepted as verify_tree gives them.  See nt_cache_compact."""
+    if _recorder is None:
+        st = (_calls or _load_calls()).cache_compact(caches, table, lengths, path, accepted, stream)
+        if st is not None:
+            if st:
+                _check(st)
+            return caches
+    import torch
+    B = _rows(table, torch.int32, "table").shape[0]
+    _rows(path, torch.int32, "path")
+    structs = [_cache_struct(*c, *([None] * (4 - len(c)))) for c in caches]
+    array = (PagedCache * max(1, len(structs)))(*structs)
+    array.keep = structs                                     # (what the copies point to)
+    _check(load().nt_cache_compact(array, len(structs), table.data_ptr(), _ref(table), _integers(lengths, torch.int32, "lengths", B), path.data_ptr(), _ref(path),
+                                   _integers(accepted, torch.int32, "accepted", B), _stream_ptr(stream)))
+    return caches
 
 
 def bmm(A, B, Cout, tile=None, stream=None):

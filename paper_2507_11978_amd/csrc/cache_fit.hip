@@ -1,0 +1,191 @@
+// Pages, slots and positions of a step's new tokens, from the sequences' lengths.
+//
+// With n = lengths[b] + counts[b] sequence b wants ceil(n / page_size) pages, as many as a table row has entries at most, and has held[b].  What it has beyond that goes back
+// onto the stack of free pages, what it lacks comes from the stack's top: surplus page number a of all (counted by sequence, then entry) lands at top - 1 - a, and missing
+// page number k is taken from top - 1 - k, where top counts the returned pages in.  Sums of counts, surplus and missing pages before a sequence are three scans.
+//
+// One workgroup does it, a sequence to a thread, 1024 at a time; the pages that move are dealt out to all threads (a bisection tells whose each is), so that a long prompt's
+// pages are not one thread's.  Then a thread to a token.
+#include "gemm_fast.h"
+#include "kernels.h"
+#include "paged_index.h"
+
+namespace nt {
+
+constexpr int kFitThreads = 1024, kFitHere = 4096;                        // (tokens that the first launch gives their slots itself)
+
+struct FitArgs {
+    const int32_t *lengths, *counts;
+    int32_t *table, *held, *free_pages, *free_count, *starts, *new_lengths, *positions;
+    int64_t *slots;
+    int64_t t_sb, tokens, capacity;
+    int32_t B, width;
+    Divider page;
+};
+
+struct Need {
+    int32_t count, after, want, held;
+};
+
+__device__ __forceinline__ Need need_of(const FitArgs &g, int32_t b)
+{
+    if (b >= g.B) return Need{0, 0, 0, 0};
+    const int32_t n = g.lengths[b] > 0 ? g.lengths[b] : 0, m = g.counts[b] > 0 ? g.counts[b] : 0;
+    const int32_t after = m < 0x7fffffff - n ? n + m : 0x7fffffff;
+    const int32_t pages = after ? (int32_t)divide(after - 1, g.page) + 1 : 0;
+    return Need{after - n, after, pages < g.width ? pages : g.width, clamp_i32(g.held[b], 0, g.width)};
+}
+
+// Sum of the threads' values before this one's; *total: of all
+__device__ __forceinline__ int64_t sum_before(int64_t v, int64_t *scratch, int64_t *total)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int64_t upto = v;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t other = __shfl_up(upto, d, 64);
+        if (lane >= d) upto += other;
+    }
+    __syncthreads();                                                       // (what was there has been read)
+    if (lane == 63) scratch[wave] = upto;
+    __syncthreads();
+    int64_t before = 0, all = 0;
+#pragma unroll
+    for (int w = 0; w < kFitThreads / 64; ++w) {
+        if (w < wave) before += scratch[w];
+        all += scratch[w];
+    }
+    *total = all;
+    return before + upto - v;
+}
+
+// The last of 1024 ascending numbers, the first of them 0, that is not above j (0 <= j)
+__device__ __forceinline__ int whose(const int64_t *first, int64_t j)
+{
+    int at = 0;
+#pragma unroll
+    for (int step = kFitThreads / 2; step; step >>= 1)
+        if (first[at + step] <= j) at += step;
+    return at;
+}
+
+__device__ __forceinline__ void place_token(const FitArgs &g, int64_t t)
+{
+    int64_t slot = -1;
+    int32_t pos = 0;
+    if (t < g.starts[g.B]) {
+        int32_t b = 0;                                                     // the last sequence that begins at or before the token
+        for (int32_t up = g.B; up - b > 1;) {
+            const int32_t at = b + (up - b) / 2;
+            if (g.starts[at] <= t) b = at;
+            else up = at;
+        }
+        pos = g.new_lengths[b] - g.starts[b + 1] + (int32_t)t;
+        const uint32_t entry = divide(pos, g.page);
+        const int32_t id = entry < (uint32_t)g.held[b] ? g.table[b * g.t_sb + entry] : -1;
+        if (id >= 0) slot = (int64_t)id * g.page.d + (pos - entry * g.page.d);
+    }
+    g.slots[t] = slot;
+    g.positions[t] = pos;
+}
+
+__global__ __launch_bounds__(kFitThreads) void cache_fit_kernel(const FitArgs g)
+{
+    __shared__ int64_t scratch[kFitThreads / 64], first[kFitThreads];
+    __shared__ int32_t from[kFitThreads];
+    const int tid = threadIdx.x;
+    int64_t back = 0, taken = 0;
+    for (int32_t c = 0; c < g.B; c += kFitThreads) {
+        const Need n = need_of(g, c + tid);
+        int64_t all;
+        sum_before(n.held > n.want ? n.held - n.want : 0, scratch, &all);
+        back += all;
+    }
+    const int64_t top = (int64_t)clamp_i32(*g.free_count, 0, (int32_t)g.capacity) + back;
+
+    // ---- pages that go back
+    int64_t done = 0;
+    for (int32_t c = 0; c < g.B; c += kFitThreads) {
+        const Need n = need_of(g, c + tid);
+        int64_t all;
+        first[tid] = sum_before(n.held > n.want ? n.held - n.want : 0, scratch, &all);
+        from[tid] = n.want;
+        __syncthreads();
+        for (int64_t j = tid; j < all; j += kFitThreads) {
+            const int s = whose(first, j);
+            const int64_t at = top - 1 - (done + j);
+            if (at < g.capacity) g.free_pages[at] = g.table[(c + s) * g.t_sb + from[s] + (j - first[s])];
+        }
+        done += all;
+        __syncthreads();
+    }
+
+    // ---- pages that are taken, and what the sequences have then
+    int64_t tokens = 0;
+    for (int32_t c = 0; c < g.B; c += kFitThreads) {
+        const Need n = need_of(g, c + tid);
+        const int32_t lacks = n.want > n.held ? n.want - n.held : 0;
+        int64_t all, sum;
+        const int64_t start = tokens + sum_before(n.count, scratch, &sum);
+        const int64_t before = sum_before(lacks, scratch, &all);
+        first[tid] = before;
+        from[tid] = n.held;
+        __syncthreads();
+        for (int64_t j = tid; j < all; j += kFitThreads) {
+            const int s = whose(first, j);
+            const int64_t at = top - 1 - (taken + j);
+            g.table[(c + s) * g.t_sb + from[s] + (j - first[s])] = at >= 0 && at < g.capacity ? g.free_pages[at] : -1;
+        }
+        if (c + tid < g.B) {
+            const int64_t left = top - taken - before;                     // pages there are for this sequence
+            g.held[c + tid] = (n.held < n.want ? n.held : n.want) + (int32_t)(left <= 0 ? 0 : left < lacks ? left : lacks);
+            g.new_lengths[c + tid] = n.after;
+            g.starts[c + tid] = (int32_t)(start < 0x7fffffff ? start : 0x7fffffff);
+        }
+        taken += all;
+        tokens += sum;
+        __syncthreads();
+    }
+    if (tid == 0) {
+        const int64_t left = top - taken;
+        *g.free_count = (int32_t)(left > g.capacity ? g.capacity : left < -0x7fffffff ? -0x7fffffff : left);
+        g.starts[g.B] = (int32_t)(tokens < 0x7fffffff ? tokens : 0x7fffffff);
+    }
+    if (g.tokens > kFitHere) return;
+    __syncthreads();
+    for (int64_t t = tid; t < g.tokens; t += kFitThreads) place_token(g, t);
+}
+
+__global__ __launch_bounds__(256) void cache_slots_kernel(const FitArgs g)
+{
+    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (t < g.tokens) place_token(g, t);
+}
+
+nt_status launch_cache_fit(const int32_t *lengths, const int32_t *counts, int64_t sequences, int64_t page_size, int32_t *table, const nt_tensor_desc *dt, int32_t *held,
+                           int32_t *free_pages, int64_t capacity, int32_t *free_count, int32_t *starts, int32_t *new_lengths, int64_t *slots, int32_t *positions,
+                           int64_t tokens, void *stream)
+{
+    if (!dt) return fail(NT_ERR_INVALID_ARG, "null tensor descriptor");
+    if (dt->ndim != 2) return fail(NT_ERR_SHAPE_MISMATCH, "the page table must be 2-D [sequences, entries]");
+    if (sequences < 0 || capacity < 0 || tokens < 0 || dt->size[0] < 0 || dt->size[1] < 0) return fail(NT_ERR_INVALID_ARG, "negative size");
+    if (dt->size[0] != sequences) return fail(NT_ERR_SHAPE_MISMATCH, "lengths and page table differ in sequences");
+    if (dt->size[1] > 1 && dt->stride[1] != 1) return fail(NT_ERR_UNSUPPORTED, "the page table needs unit stride along a sequence");
+    if (page_size < 1 || page_size > (1 << 24)) return fail(NT_ERR_UNSUPPORTED, "page_size must be 1 to 2^24");
+    if (sequences > (1 << 24) || dt->size[1] > 0x7fffffffLL) return fail(NT_ERR_UNSUPPORTED, "page table too large");
+    if (capacity > 0x7fffffffLL) return fail(NT_ERR_UNSUPPORTED, "more than 2^31 - 1 pages");
+    if (tokens > 0x7fffffffLL) return fail(NT_ERR_UNSUPPORTED, "more than 2^31 - 1 tokens");
+    if (!starts || !free_count || (sequences && (!lengths || !counts || !held || !new_lengths)) || (sequences && dt->size[1] && !table) || (capacity && !free_pages) ||
+        (tokens && (!slots || !positions)))
+        return fail(NT_ERR_INVALID_ARG, "null device pointer");
+    const FitArgs a{lengths, counts, table, held, free_pages, free_count, starts, new_lengths, positions, slots, dt->stride[0], tokens, capacity,
+                    (int32_t)sequences, (int32_t)dt->size[1], divider_of((uint32_t)page_size)};
+    hipStream_t s = (hipStream_t)stream;
+    hipLaunchKernelGGL(cache_fit_kernel, dim3(1), dim3(kFitThreads), 0, s, a);
+    const nt_status st = check_launch("cache_fit_kernel");
+    if (st != NT_OK || tokens <= kFitHere) return st;
+    hipLaunchKernelGGL(cache_slots_kernel, dim3((unsigned)((tokens + 255) / 256)), dim3(256), 0, s, a);
+    return check_launch("cache_slots_kernel");
+}
+
+}  // namespace nt

@@ -100,9 +100,27 @@ nt_status launch_sdpa_desc(const void *q, const nt_tensor_desc *dq, const void *
 // paged key / value cache: writing / reading it, and attention over it
 nt_status launch_cache(bool write, const nt_paged_cache *c, const void *k, const nt_tensor_desc *dk, const void *v, const nt_tensor_desc *dv,
                        const int64_t *slots, int dtype, void *stream);
+// of a tree's tokens: who sees whom, and (windows) how far they are from the root
+struct TreeMasks {
+    const uint64_t *masks;
+    const nt_tensor_desc *d;
+    const int32_t *depths;
+};
 nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_paged_cache *c, const int32_t *table, const nt_tensor_desc *dt,
                             const int32_t *starts, const int32_t *lengths, void *out, const nt_tensor_desc *dout,
-                            float scale, int causal, int64_t window, int64_t max_queries, int64_t max_length, int dtype, void *stream);
+                            float scale, int causal, int64_t window, int64_t max_queries, int64_t max_length, int dtype, void *stream,
+                            const TreeMasks *tree = nullptr);
+// drafted tokens: pages and slots, trees' masks, verification, and the accepted tokens' move
+nt_status launch_cache_fit(const int32_t *lengths, const int32_t *counts, int64_t sequences, int64_t page_size, int32_t *table, const nt_tensor_desc *dt, int32_t *held,
+                           int32_t *free_pages, int64_t capacity, int32_t *free_count, int32_t *starts, int32_t *new_lengths, int64_t *slots, int32_t *positions,
+                           int64_t tokens, void *stream);
+nt_status launch_cache_compact(const nt_paged_cache *caches, int64_t n, const int32_t *table, const nt_tensor_desc *dt, const int32_t *lengths, const int32_t *path,
+                               const nt_tensor_desc *dp, const int32_t *accepted, void *stream);
+nt_status launch_tree_masks(const int32_t *parents, const int32_t *starts, int64_t sequences, uint64_t *masks, const nt_tensor_desc *dm, int32_t *depths,
+                            const int32_t *lengths, int32_t *positions, int64_t window, void *stream);
+nt_status launch_verify_tree(const void *target, const nt_tensor_desc *dt, const void *draft, const nt_tensor_desc *dd, const int64_t *ids, const int32_t *parents,
+                             const int32_t *starts, int64_t sequences, const float *uniform, const float *last_uniform, int32_t *path, const nt_tensor_desc *dp,
+                             int32_t *accepted, int64_t *next, const int32_t *lengths, int32_t *new_lengths, int dtype, void *stream);
 nt_status check_cache(const nt_paged_cache *c, int dtype, int *kind);     // kind: a CacheKind
 const nt_paged_plan &last_paged_plan();
 

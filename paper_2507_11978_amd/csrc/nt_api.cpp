@@ -644,6 +644,43 @@ nt_status nt_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_paged_
     return nt::launch_sdpa_paged(q, dq, cache, table, d_table, starts, lengths, out, dout, scale, causal, window, max_queries, max_length, dtype, hip_stream);
 }
 
+nt_status nt_sdpa_paged_tree(const void *q, const nt_tensor_desc *dq, const nt_paged_cache *cache, const int32_t *table, const nt_tensor_desc *d_table,
+                             const int32_t *starts, const int32_t *lengths, const uint64_t *masks, const nt_tensor_desc *d_masks, const int32_t *depths,
+                             void *out, const nt_tensor_desc *dout, float scale, int64_t window, int64_t max_queries, int64_t max_length, nt_dtype dtype, void *hip_stream)
+{
+    const nt::TreeMasks tree{masks, d_masks, depths};
+    return nt::launch_sdpa_paged(q, dq, cache, table, d_table, starts, lengths, out, dout, scale, 1, window, max_queries, max_length, dtype, hip_stream, &tree);
+}
+
+nt_status nt_cache_fit(const int32_t *lengths, const int32_t *counts, int64_t sequences, int64_t page_size, int32_t *table, const nt_tensor_desc *d_table,
+                       int32_t *held, int32_t *free_pages, int64_t capacity, int32_t *free_count, int32_t *starts, int32_t *new_lengths,
+                       int64_t *slots, int32_t *positions, int64_t tokens, void *hip_stream)
+{
+    return nt::launch_cache_fit(lengths, counts, sequences, page_size, table, d_table, held, free_pages, capacity, free_count, starts, new_lengths, slots, positions,
+                                tokens, hip_stream);
+}
+
+nt_status nt_tree_masks(const int32_t *parents, const int32_t *starts, int64_t sequences, uint64_t *masks, const nt_tensor_desc *d_masks, int32_t *depths,
+                        const int32_t *lengths, int32_t *positions, int64_t window, void *hip_stream)
+{
+    return nt::launch_tree_masks(parents, starts, sequences, masks, d_masks, depths, lengths, positions, window, hip_stream);
+}
+
+nt_status nt_verify_tree(const void *target, const nt_tensor_desc *d_target, const void *draft, const nt_tensor_desc *d_draft, const int64_t *ids,
+                         const int32_t *parents, const int32_t *starts, int64_t sequences, const float *uniform, const float *last_uniform,
+                         int32_t *path, const nt_tensor_desc *d_path, int32_t *accepted, int64_t *next, const int32_t *lengths, int32_t *new_lengths,
+                         nt_dtype dtype, void *hip_stream)
+{
+    return nt::launch_verify_tree(target, d_target, draft, d_draft, ids, parents, starts, sequences, uniform, last_uniform, path, d_path, accepted, next, lengths,
+                                  new_lengths, dtype, hip_stream);
+}
+
+nt_status nt_cache_compact(const nt_paged_cache *caches, int64_t n_caches, const int32_t *table, const nt_tensor_desc *d_table, const int32_t *lengths,
+                           const int32_t *path, const nt_tensor_desc *d_path, const int32_t *accepted, void *hip_stream)
+{
+    return nt::launch_cache_compact(caches, n_caches, table, d_table, lengths, path, d_path, accepted, hip_stream);
+}
+
 nt_status nt_last_paged_plan(nt_paged_plan *out)
 {
     if (!out) return fail(NT_ERR_INVALID_ARG, "null output pointer");
@@ -721,6 +758,6 @@ nt_status nt_mfma_probe(const void *data, int64_t n_elems, nt_dtype dtype, int32
 
 const char *nt_last_error(void) { return nt::last_error().c_str(); }
 
-const char *nt_version(void) { return "nt-mi355x 0.8 (gfx950)"; }
+const char *nt_version(void) { return "nt-mi355x 0.9 (gfx950)"; }
 
 }  // extern "C"

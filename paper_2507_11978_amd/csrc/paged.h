@@ -192,6 +192,11 @@ struct PagedArgs {
     int32_t aligned;                   // every row of the cache begins at a multiple of 16 bytes
     int32_t splits, split_keys;        // the keys of a tile are shared out over `splits` programs, split_keys each (the last: what is left)
     Divider page, group;               // by page_size, by G
+    // trees of drafted tokens: a row of `words` words for each token, and its depth (windows)
+    const uint64_t *masks;
+    const int32_t *depths;
+    int64_t m_st;
+    int32_t words;
     float scale_log2e;                 // scale * log2(e): exponentials are taken in base 2
     // one program's share of a row (splits > 1): [token * Hq + head][split] of (reference, sum), and of D unnormalised outputs
     float *part_ml, *part_o;
@@ -202,6 +207,11 @@ __device__ __forceinline__ Sequence sequence_of(const PagedArgs &g, int b) { ret
 __device__ __forceinline__ KeyRange keys_of(const PagedArgs &g, const Sequence &q, int32_t i0, int32_t i1, int split, int32_t block)
 {
     return key_range(q, i0, i1, g.causal, g.window, split, g.splits, g.split_keys, block, g.width * (int32_t)g.page.d);
+}
+
+__device__ __forceinline__ KeyRange tree_keys_of(const PagedArgs &g, const Sequence &q, int split, int32_t block)
+{
+    return tree_range(q, g.window, split, g.splits, g.split_keys, block, g.width * (int32_t)g.page.d);
 }
 
 // ---- where a block of keys lies in LDS: rows of SIZE 16-bit elements, their 16-byte chunks in an order that depends on the row, such that 16
@@ -229,5 +239,8 @@ constexpr uint32_t kNanPair = 0x7fff7fffu;
 nt_status launch_paged_64(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream);
 nt_status launch_paged_128(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream);
 nt_status launch_paged_256(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream);
+nt_status launch_paged_tree_64(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream);
+nt_status launch_paged_tree_128(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream);
+nt_status launch_paged_tree_256(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream);
 
 }  // namespace nt

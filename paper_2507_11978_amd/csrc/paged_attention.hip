@@ -111,7 +111,7 @@ const nt_paged_plan &last_paged_plan() { return t_paged; }
 
 nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_paged_cache *c, const int32_t *table, const nt_tensor_desc *dt,
                             const int32_t *starts, const int32_t *lengths, void *out, const nt_tensor_desc *dout,
-                            float scale, int causal, int64_t window, int64_t max_queries, int64_t max_length, int dtype, void *stream)
+                            float scale, int causal, int64_t window, int64_t max_queries, int64_t max_length, int dtype, void *stream, const TreeMasks *tree)
 {
     t_paged = nt_paged_plan{};
     int kind = CACHE_SAME;
@@ -134,7 +134,16 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     if (!(scale == scale)) return fail(NT_ERR_INVALID_ARG, "scale is NaN");
     if (T > (1 << 30) / Hq) return fail(NT_ERR_UNSUPPORTED, "tokens * query heads must be at most 2^30");
     if (W > 0x7fffffffLL || B > (1 << 24)) return fail(NT_ERR_UNSUPPORTED, "page table too large");
+    if (tree) {
+        if (!tree->d) return fail(NT_ERR_INVALID_ARG, "null tensor descriptor");
+        if (tree->d->ndim != 2) return fail(NT_ERR_SHAPE_MISMATCH, "masks must be 2-D [tokens, words]");
+        if (tree->d->size[0] != T) return fail(NT_ERR_SHAPE_MISMATCH, "queries and masks differ in tokens");
+        if (tree->d->size[1] < 1 || tree->d->size[1] > (1 << 20)) return fail(NT_ERR_UNSUPPORTED, "masks must have 1 to 2^20 words");
+        if (tree->d->size[1] > 1 && tree->d->stride[1] != 1) return fail(NT_ERR_UNSUPPORTED, "masks need unit stride along a token's words");
+        if (window && !tree->depths) return fail(NT_ERR_INVALID_ARG, "a window needs the tokens' depths");
+    }
     if (T == 0 || B == 0) return NT_OK;
+    if (tree && !tree->masks) return fail(NT_ERR_INVALID_ARG, "null device pointer");
     if (!q || !out || !starts || !lengths || (W && !table)) return fail(NT_ERR_INVALID_ARG, "null device pointer");
     if (pages == 0) return fail(NT_ERR_INVALID_ARG, "the cache has no pages");
 
@@ -161,6 +170,10 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     a.near = a.k_ss >= 0 && a.k_ss < most_bytes / (16 * es) && a.v_ss >= 0 && a.v_ss < most_bytes / (16 * es);
     a.uniform = a.near && page_size % 16 == 0;
     a.aligned = (((uintptr_t)a.K | (uintptr_t)a.V | (uint64_t)((a.k_sp | a.k_ss | a.k_sh | a.v_sp | a.v_ss | a.v_sh) * es)) & 15) == 0;
+    if (tree) {
+        a.masks = tree->masks; a.depths = tree->depths;
+        a.m_st = tree->d->stride[0]; a.words = (int32_t)tree->d->size[1];
+    }
     a.page = divider_of((uint32_t)page_size);
     a.group = divider_of((uint32_t)a.G);
     a.scale_log2e = (scale == 0.f ? 1.0f / sqrtf((float)D) : scale) * 1.4426950408889634f;
@@ -207,7 +220,8 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     a.splits = (int32_t)splits;
     a.split_keys = (int32_t)std::min<int64_t>(share, 0x7fffffff / 2);
     const bool bf16 = dtype == NT_BF16;
-    auto launch = built == 64 ? launch_paged_64 : built == 128 ? launch_paged_128 : launch_paged_256;
+    auto launch = built == 64 ? (tree ? launch_paged_tree_64 : launch_paged_64) : built == 128 ? (tree ? launch_paged_tree_128 : launch_paged_128)
+                                                                                          : (tree ? launch_paged_tree_256 : launch_paged_256);
     nt_status rc = launch(a, rows, base * splits, bf16, kind, stream);
     if (rc != NT_OK) return rc;
     if (splits > 1) {

@@ -74,6 +74,54 @@ NT_HD KeyRange key_range(const Sequence &q, int32_t i0, int32_t i1, int32_t caus
     return KeyRange{lo, hi < lo ? lo : hi};
 }
 
+// ---- trees of drafted tokens: token i sees the positions before the new ones, `past` = length - count of them (a window: the last ones, counted from past + its
+// depth), and of position past + k it sees what bit k of its mask says.
+
+// bits [from, to) of 64
+NT_HD uint64_t bits_between(int32_t from, int32_t to)
+{
+    const uint64_t below = from <= 0 ? 0ull : from >= 64 ? ~0ull : (1ull << from) - 1, under = to <= 0 ? 0ull : to >= 64 ? ~0ull : (1ull << to) - 1;
+    return under & ~below;
+}
+
+// 64 bits of a mask of `words` words, from bit `at` on (before the first bit and behind the last there are zeros)
+NT_HD uint64_t bits_from(const uint64_t *mask, int32_t words, int32_t at)
+{
+    const int32_t w = at >> 6, s = at & 63;
+    const uint64_t lo = (uint32_t)w < (uint32_t)words ? mask[w] : 0, hi = s && (uint32_t)(w + 1) < (uint32_t)words ? mask[w + 1] : 0;
+    return s ? lo >> s | hi << (64 - s) : lo;
+}
+
+// The first position that a token of this depth (0 to count - 1) sees of the past
+NT_HD int32_t tree_row_lo(int32_t past, int32_t count, int32_t depth, int32_t window)
+{
+    const int64_t lo = (int64_t)past + clamp_i32(depth, 0, count - 1) - window + 1;
+    return window && lo > 0 ? (int32_t)(lo < past ? lo : past) : 0;
+}
+
+// Which of the 64 positions from `base` (0 <= base < length) on the token sees; row_lo: as above
+NT_HD uint64_t tree_keys(const uint64_t *mask, int32_t words, int32_t base, int32_t row_lo, int32_t past, int32_t length)
+{
+    const uint64_t before = past > 0 ? bits_between(row_lo > base ? (row_lo - base < 64 ? row_lo - base : 64) : 0, past > base ? (past - base < 64 ? past - base : 64) : 0) : 0;
+    if (past >= 64 && base <= past - 64) return before;
+    const int32_t first = past - base, end = length - base < 64 ? length - base : 64;             // (base < length <= past + new tokens: both fit)
+    return before | (bits_from(mask, words, -first) & bits_between(first, end));
+}
+
+// The keys that a program of a tree's rows walks: all that some token may see, or share number `split` of them (as key_range).  Where the past passes what the table
+// reaches, whoever sees anything sees a position without a page among the last of the past and the new ones: no others are needed to show it.
+NT_HD KeyRange tree_range(const Sequence &q, int32_t window, int split, int splits, int32_t share_keys, int32_t block, int32_t capacity)
+{
+    const int32_t past = q.length - q.count;
+    int32_t lo = past > capacity ? past - 1 : window && past >= window ? past - window + 1 : 0, hi = q.length;
+    if (splits > 1) {
+        const int64_t base = lo / block * block, from = base + (int64_t)split * share_keys, to = from + share_keys;
+        if (split > 0 && from > lo) lo = from > hi ? hi : (int32_t)from;
+        if (split + 1 < splits && to < hi) hi = (int32_t)to;
+    }
+    return KeyRange{lo, hi < lo ? lo : hi};
+}
+
 // The page of a position, in two steps: its entry of the table row is on its way long before the page is needed.
 // Which entry is read for number `index`: past the row's end its last, which is not used then (of a row without entries the first: the launcher puts something
 // to read in its place)

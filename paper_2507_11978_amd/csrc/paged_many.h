@@ -41,7 +41,8 @@ constexpr size_t many_lds(int size) { return 4 * many_block(size) + 2 * 2 * many
 constexpr int many_resident(int kind, int size) { return size == 256 ? 1 : size == 128 || kind != CACHE_SAME ? 2 : 3; }
 
 // FULL: rows of SIZE elements (the switched-off lanes of others cost 5 % where none is: 1024 queries x 8000 keys x 32/8 heads x 128 bf16 217 us, 228)
-template <bool BF16, int KIND, int SIZE, bool FAST, bool FULL>
+// TREE: as in paged_few.h
+template <bool BF16, int KIND, int SIZE, bool FAST, bool FULL, bool TREE>
 __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void paged_many_kernel(const PagedArgs g)
 {
     constexpr bool DMA = FAST && KIND == CACHE_SAME;
@@ -80,20 +81,23 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
     const int32_t *pages = g.table + (int64_t)b * g.t_sb;
     const char *Kh = g.K + (int64_t)h * g.k_sh * ES, *Vh = g.V + (int64_t)h * g.v_sh * ES;
     const int32_t tile_i0 = (int32_t)divide(r0, g.group), tile_i1 = (int32_t)divide(tile_last, g.group);
-    const KeyRange keys = keys_of(g, seq, tile_i0, tile_i1, split, KB);
-    // keys that every row of the tile sees: [seen_lo, seen_hi)
-    const int32_t seen_lo = keys_seen(seq, tile_i1, g.causal, g.window).lo, seen_hi = keys_seen(seq, tile_i0, g.causal, g.window).hi;
+    const KeyRange keys = TREE ? tree_keys_of(g, seq, split, KB) : keys_of(g, seq, tile_i0, tile_i1, split, KB);
+    // keys that every row of the tile sees: [seen_lo, seen_hi) (a tree's rows: no token is deeper than their count)
+    const int32_t past = seq.length - seq.count;
+    const int32_t seen_lo = TREE ? tree_row_lo(past, seq.count, seq.count, g.window) : keys_seen(seq, tile_i1, g.causal, g.window).lo;
+    const int32_t seen_hi = TREE ? past : keys_seen(seq, tile_i0, g.causal, g.window).hi;
 
     // ---- this lane's row and its keys [row_lo, row_hi); the wavefront's: seen by some row [wave_lo, wave_hi), by all [all_lo, all_hi)
     const int row = r0 + 32 * wave + l32;
     const bool real = row < rows_all;
     const bool busy = r0 + 32 * wave < rows_all;                           // wavefront-uniform
     const uint32_t rc = real ? row : tile_last, mine = divide(rc, g.group), head = h * g.G + (rc - mine * g.group.d);
-    const KeyRange row_keys = keys_seen(seq, (int32_t)mine, g.causal, g.window);
-    const int32_t row_lo = row_keys.lo, row_hi = row_keys.hi;
-    const int32_t all_lo = __builtin_amdgcn_readlane(row_lo, 31), all_hi = __builtin_amdgcn_readlane(row_hi, 0);
-    const int32_t wave_lo = __builtin_amdgcn_readlane(row_lo, 0), wave_hi = __builtin_amdgcn_readlane(row_hi, 31);
     const int64_t token = seq.first + (int32_t)mine;
+    const KeyRange row_keys = TREE ? KeyRange{tree_row_lo(past, seq.count, g.window ? g.depths[token] : 0, g.window), past} : keys_seen(seq, (int32_t)mine, g.causal, g.window);
+    const int32_t row_lo = row_keys.lo, row_hi = row_keys.hi;
+    const int32_t all_lo = TREE ? seen_lo : __builtin_amdgcn_readlane(row_lo, 31), all_hi = TREE ? past : __builtin_amdgcn_readlane(row_hi, 0);
+    const int32_t wave_lo = TREE ? keys.lo : __builtin_amdgcn_readlane(row_lo, 0), wave_hi = TREE ? keys.hi : __builtin_amdgcn_readlane(row_hi, 31);
+    auto row_bits = [&](int base) { return tree_keys(g.masks + token * g.m_st, g.words, base, row_lo, past, seq.length); };        // (TREE) of the keys from `base` on
 
     u32x4 qf[SIZE / 16];
     {
@@ -293,7 +297,17 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
                 }
         }
         const bool hidden = base < all_lo || base + KB > all_hi;          // wavefront-uniform: from some row
-        if (hidden) {
+        uint64_t vis = ~0ull;                                              // (TREE: which keys of the block the row sees, from key 4 hi on)
+        if constexpr (TREE) {
+            if (hidden) {
+                const float out = g.scale_log2e >= 0.f ? -INFINITY : INFINITY;
+                vis = row_bits(base) >> (4 * hi);
+#pragma unroll
+                for (int jb = 0; jb < JB; ++jb)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) st[jb][v] = (vis >> (32 * jb + 8 * (v / 4) + v % 4)) & 1 ? st[jb][v] : out;
+            }
+        } else if (hidden) {
             const float out = g.scale_log2e >= 0.f ? -INFINITY : INFINITY;
             const uint32_t from = here(base + 4 * hi) - row_lo, count = row_hi > row_lo ? row_hi - row_lo : 0;      // (keys before row_lo: far beyond count)
 #pragma unroll
@@ -381,7 +395,16 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
             pending = __any(m_new == -INFINITY);
         }
         l_run += rs;
-        if (KIND != CACHE_SAME && hidden) {                                // (the scale of a hidden key may be anything; a seen one's NaN shows whatever its weight)
+        if constexpr (TREE && KIND != CACHE_SAME) {
+            if (hidden) {
+#pragma unroll
+                for (int i = 0; i < 8 * JB; ++i) {
+                    const uint32_t two = (uint32_t)(vis >> (8 * (i / 2) + 2 * (i % 2))) & 3, seen = (two & 1 ? 0xffffu : 0u) | (two & 2 ? 0xffff0000u : 0u);
+                    pk[i / 8][i / 4 % 2][i % 4] &= seen;
+                    if constexpr (SPLIT) rest[i / 8][i / 4 % 2][i % 4] &= seen;
+                }
+            }
+        } else if (KIND != CACHE_SAME && hidden) {                         // (the scale of a hidden key may be anything; a seen one's NaN shows whatever its weight)
             const uint32_t from = here(base + 4 * hi) - row_lo, count = row_hi > row_lo ? row_hi - row_lo : 0;
 #pragma unroll
             for (int i = 0; i < 8 * JB; ++i) {                             // pair i: key 8 (i / 2) + 4 hi + 2 (i % 2) of the block and the next
@@ -418,9 +441,10 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
     auto add_not_finite = [&](const int kb, const uint32_t copy) {
         const char *vs_lds = smem + (2 + copy) * BLK;
         const int half = here(hi);
+        const uint64_t vis = TREE ? row_bits(kb * KB) : 0;
 #pragma unroll 1
         for (int j = 0; j < KB; ++j) {
-            const bool sees = kb * KB + j >= row_lo && kb * KB + j < row_hi;
+            const bool sees = TREE ? (vis >> j) & 1 : kb * KB + j >= row_lo && kb * KB + j < row_hi;
 #pragma unroll
             for (int db = 0; db < SIZE / 32; ++db)
 #pragma unroll

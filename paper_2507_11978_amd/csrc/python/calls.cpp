@@ -11,6 +11,8 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <vector>
+
 #include "../../../include/nt.h"
 #include "without_lock.h"
 
@@ -29,6 +31,11 @@ decltype(&nt_silu) p_silu;
 decltype(&nt_cache_write) p_cache_write;
 decltype(&nt_cache_read) p_cache_read;
 decltype(&nt_sdpa_paged) p_sdpa_paged;
+decltype(&nt_sdpa_paged_tree) p_sdpa_paged_tree;
+decltype(&nt_cache_fit) p_cache_fit;
+decltype(&nt_tree_masks) p_tree_masks;
+decltype(&nt_verify_tree) p_verify_tree;
+decltype(&nt_cache_compact) p_cache_compact;
 
 struct Operand {
     void *p;
@@ -346,16 +353,137 @@ PyObject *sdpa_paged(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// sdpa_paged_tree(q, k_cache, v_cache, table, starts, lengths, masks, out, k_scale, v_scale, depths, scale, window, max_queries, max_length, stream)
+PyObject *sdpa_paged_tree(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        Operand q, table, starts, lengths, masks, depths, o;
+        Paged c;
+        float scale;
+        int64_t window, queries, length;
+        void *s;
+        depths.p = nullptr;
+        if (!p_sdpa_paged_tree || n != 16 || !take(a[0], &q) || !take_paged(a[1], a[2], a[8], a[9], &c) || !take_integers(a[3], at::kInt, 2, &table) ||
+            !take_list(a[4], at::kInt, table.d.size[0] + 1, &starts) || !take_list(a[5], at::kInt, table.d.size[0], &lengths) ||
+            !take_integers(a[6], at::kLong, 2, &masks) || !take(a[7], &o) || o.dtype != q.dtype ||
+            (a[10] != Py_None && !take_list(a[10], at::kInt, q.d.size[0], &depths)) || !real(a[11], &scale) || !long_integer(a[12], &window) ||
+            !long_integer(a[13], &queries) || !long_integer(a[14], &length) || !stream_of(a[15], &s))
+            return declined();
+        return without_lock([&] {
+            return p_sdpa_paged_tree(q.p, &q.d, &c.c, (const int32_t *)table.p, &table.d, (const int32_t *)starts.p, (const int32_t *)lengths.p,
+                                     (const uint64_t *)masks.p, &masks.d, (const int32_t *)depths.p, o.p, &o.d, scale, window, queries, length, q.dtype, s);
+        });
+    });
+}
+
+// cache_fit(lengths, counts, page_size, table, held, free_pages, free_count, starts, new_lengths, slots, positions, stream)
+PyObject *cache_fit(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        Operand lengths, counts, table, held, pages, count, starts, after, slots, positions;
+        int64_t page;
+        void *s;
+        if (!p_cache_fit || n != 12 || !take_integers(a[3], at::kInt, 2, &table) || !take_integers(a[5], at::kInt, 1, &pages) || !take_integers(a[9], at::kLong, 1, &slots))
+            return declined();
+        const int64_t B = table.d.size[0], capacity = pages.d.size[0], T = slots.d.size[0];
+        if (!take_list(a[0], at::kInt, B, &lengths) || !take_list(a[1], at::kInt, B, &counts) || !long_integer(a[2], &page) || !take_list(a[4], at::kInt, B, &held) ||
+            !take_list(a[5], at::kInt, capacity, &pages) || !take_list(a[6], at::kInt, 1, &count) || !take_list(a[7], at::kInt, B + 1, &starts) ||
+            !take_list(a[8], at::kInt, B, &after) || !take_list(a[9], at::kLong, T, &slots) || !take_list(a[10], at::kInt, T, &positions) || !stream_of(a[11], &s))
+            return declined();
+        return without_lock([&] {
+            return p_cache_fit((const int32_t *)lengths.p, (const int32_t *)counts.p, B, page, (int32_t *)table.p, &table.d, (int32_t *)held.p, (int32_t *)pages.p, capacity,
+                               (int32_t *)count.p, (int32_t *)starts.p, (int32_t *)after.p, (int64_t *)slots.p, (int32_t *)positions.p, T, s);
+        });
+    });
+}
+
+// tree_masks(parents, starts, masks, depths, lengths, positions, window, stream)
+PyObject *tree_masks(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        Operand parents, starts, masks, depths, lengths, positions;
+        int64_t window;
+        void *s;
+        lengths.p = positions.p = nullptr;
+        if (!p_tree_masks || n != 8 || !take_integers(a[2], at::kLong, 2, &masks) || !take_integers(a[1], at::kInt, 1, &starts)) return declined();
+        const int64_t T = masks.d.size[0], B = starts.d.size[0] - 1;
+        if (B < 0 || !take_list(a[0], at::kInt, T, &parents) || !take_list(a[1], at::kInt, B + 1, &starts) || !take_list(a[3], at::kInt, T, &depths) ||
+            (a[4] != Py_None && !take_list(a[4], at::kInt, B, &lengths)) || (a[5] != Py_None && !take_list(a[5], at::kInt, T, &positions)) ||
+            (a[4] == Py_None) != (a[5] == Py_None) || !long_integer(a[6], &window) || !stream_of(a[7], &s))
+            return declined();
+        return without_lock([&] {
+            return p_tree_masks((const int32_t *)parents.p, (const int32_t *)starts.p, B, (uint64_t *)masks.p, &masks.d, (int32_t *)depths.p, (const int32_t *)lengths.p,
+                                (int32_t *)positions.p, window, s);
+        });
+    });
+}
+
+// verify_tree(target, draft, ids, parents, starts, uniform, last_uniform, path, accepted, next, lengths, new_lengths, stream)
+PyObject *verify_tree(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        Operand target, draft, ids, parents, starts, uniform, last, path, accepted, next, lengths, after;
+        void *s;
+        draft.p = lengths.p = after.p = nullptr;
+        if (!p_verify_tree || n != 13 || !take(a[0], &target) || target.d.ndim != 2 || !take_integers(a[7], at::kInt, 2, &path)) return declined();
+        const int64_t T = target.d.size[0], B = path.d.size[0];
+        if ((a[1] != Py_None && (!take(a[1], &draft) || draft.dtype != target.dtype || !draft.p)) || !take_list(a[2], at::kLong, T, &ids) ||
+            !take_list(a[3], at::kInt, T, &parents) || !take_list(a[4], at::kInt, B + 1, &starts) || !take_list(a[5], at::kFloat, T, &uniform) ||
+            !take_list(a[6], at::kFloat, B, &last) || !take_list(a[8], at::kInt, B, &accepted) || !take_list(a[9], at::kLong, B, &next) ||
+            (a[10] == Py_None) != (a[11] == Py_None) || (a[10] != Py_None && (!take_list(a[10], at::kInt, B, &lengths) || !take_list(a[11], at::kInt, B, &after))) ||
+            !stream_of(a[12], &s))
+            return declined();
+        return without_lock([&] {
+            return p_verify_tree(target.p, &target.d, draft.p, draft.p ? &draft.d : nullptr, (const int64_t *)ids.p, (const int32_t *)parents.p, (const int32_t *)starts.p, B,
+                                 (const float *)uniform.p, (const float *)last.p, (int32_t *)path.p, &path.d, (int32_t *)accepted.p, (int64_t *)next.p,
+                                 (const int32_t *)lengths.p, (int32_t *)after.p, target.dtype, s);
+        });
+    });
+}
+
+// cache_compact(list of (k, v) or (k, v, k_scale, v_scale), table, lengths, path, accepted, stream)
+PyObject *cache_compact(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        Operand table, lengths, path, accepted;
+        void *s;
+        if (!p_cache_compact || n != 6 || !(PyList_CheckExact(a[0]) || PyTuple_CheckExact(a[0])) || !take_integers(a[1], at::kInt, 2, &table)) return declined();
+        const int64_t B = table.d.size[0];
+        if (!take_list(a[2], at::kInt, B, &lengths) || !take_integers(a[3], at::kInt, 2, &path) || !take_list(a[4], at::kInt, B, &accepted) || !stream_of(a[5], &s))
+            return declined();
+        const bool list = PyList_CheckExact(a[0]);
+        const Py_ssize_t m = list ? PyList_GET_SIZE(a[0]) : PyTuple_GET_SIZE(a[0]);
+        std::vector<Paged> c((size_t)m);                                   // (filled in place: the descriptions point into their own elements)
+        std::vector<nt_paged_cache> caches((size_t)m);
+        for (Py_ssize_t i = 0; i < m; ++i) {
+            PyObject *o = list ? PyList_GET_ITEM(a[0], i) : PyTuple_GET_ITEM(a[0], i);
+            const bool l = PyList_CheckExact(o);
+            if (!l && !PyTuple_CheckExact(o)) return declined();
+            const Py_ssize_t parts = l ? PyList_GET_SIZE(o) : PyTuple_GET_SIZE(o);
+            if (parts != 2 && parts != 4) return declined();
+            PyObject *part[4] = {nullptr, nullptr, Py_None, Py_None};
+            for (Py_ssize_t j = 0; j < parts; ++j) part[j] = l ? PyList_GET_ITEM(o, j) : PyTuple_GET_ITEM(o, j);
+            if (!take_paged(part[0], part[1], part[2], part[3], &c[(size_t)i])) return declined();
+            caches[(size_t)i] = c[(size_t)i].c;
+        }
+        return without_lock([&] {
+            return p_cache_compact(caches.data(), m, (const int32_t *)table.p, &table.d, (const int32_t *)lengths.p, (const int32_t *)path.p, &path.d,
+                                   (const int32_t *)accepted.p, s);
+        });
+    });
+}
+
 // bind(addresses of nt_gemm, nt_bmm, nt_addmm, nt_addmm_act, nt_conv2d_implicit, nt_sdpa, nt_softmax, nt_rms_norm, nt_add, nt_silu,
-// nt_cache_write, nt_cache_read, nt_sdpa_paged)
+// nt_cache_write, nt_cache_read, nt_sdpa_paged, nt_sdpa_paged_tree, nt_cache_fit, nt_tree_masks, nt_verify_tree, nt_cache_compact)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    if (n != 13) {
-        PyErr_SetString(PyExc_TypeError, "thirteen addresses wanted");
+    constexpr int N = 18;
+    if (n != N) {
+        PyErr_SetString(PyExc_TypeError, "eighteen addresses wanted");
         return nullptr;
     }
-    void *p[13];
-    for (int i = 0; i < 13; ++i) {
+    void *p[N];
+    for (int i = 0; i < N; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (!p[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address");
@@ -366,12 +494,15 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
     p_conv = (decltype(p_conv))p[4]; p_sdpa = (decltype(p_sdpa))p[5]; p_softmax = (decltype(p_softmax))p[6]; p_rms_norm = (decltype(p_rms_norm))p[7];
     p_add = (decltype(p_add))p[8]; p_silu = (decltype(p_silu))p[9];
     p_cache_write = (decltype(p_cache_write))p[10]; p_cache_read = (decltype(p_cache_read))p[11]; p_sdpa_paged = (decltype(p_sdpa_paged))p[12];
+    p_sdpa_paged_tree = (decltype(p_sdpa_paged_tree))p[13]; p_cache_fit = (decltype(p_cache_fit))p[14]; p_tree_masks = (decltype(p_tree_masks))p[15];
+    p_verify_tree = (decltype(p_verify_tree))p[16]; p_cache_compact = (decltype(p_cache_compact))p[17];
     Py_RETURN_NONE;
 }
 
 #define NT_CALL(NAME) {#NAME, (PyCFunction)(void (*)(void))NAME, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {NT_CALL(gemm), NT_CALL(bmm), NT_CALL(addmm), NT_CALL(conv2d), NT_CALL(sdpa), NT_CALL(softmax), NT_CALL(rms_norm),
-                         NT_CALL(add), NT_CALL(silu), NT_CALL(cache_write), NT_CALL(cache_read), NT_CALL(sdpa_paged), NT_CALL(bind), {nullptr, nullptr, 0, nullptr}};
+                         NT_CALL(add), NT_CALL(silu), NT_CALL(cache_write), NT_CALL(cache_read), NT_CALL(sdpa_paged), NT_CALL(sdpa_paged_tree), NT_CALL(cache_fit),
+                         NT_CALL(tree_masks), NT_CALL(verify_tree), NT_CALL(cache_compact), NT_CALL(bind), {nullptr, nullptr, 0, nullptr}};
 #undef NT_CALL
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_nt_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
