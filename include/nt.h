@@ -416,7 +416,12 @@ nt_status nt_tree_masks(const int32_t *parents, const int32_t *starts, int64_t s
 /* nt_sdpa_paged_tree: nt_sdpa_paged for trees.  New token i of n of sequence b sees the past, positions 0 <= j < lengths[b] - n, and of the new tokens, at positions
  * lengths[b] - n + k, those whose bit k is set in its row of masks (as nt_tree_masks makes them; any bits will do, a token need not see itself; bits of
  * numbers from n on mean nothing).  window > 0: of the past the positions j > lengths[b] - n + depths[t] - window (depths[t] is taken as 0 to n - 1; needed with a window only).
- * Everything else, a token that sees nothing or a position without a page, precision, memory, and max_queries and max_length, as nt_sdpa_paged. */
+ * What a token does not see has no part in its result; one that sees nothing, or nothing with a score above -inf, gets zeros, one that sees a position without a page NaN.
+ * Scores, weights' sums and accumulators are fp32; what multiplies V is the weight as the sum of two numbers of `dtype` (bf16 over codes), off by 2^-16 of it at most (fp16: 2^-22,
+ * or 2^-24 of a weight of 1).  max_queries (the most new tokens of a sequence, 0: not known) chooses how rows are dealt out; one that is too low costs time and is not an
+ * error.  The keys are dealt out by the lengths, which only the device needs to know: max_length is checked and not used.
+ * Memory: results of keys that are shared out (up to 1024 sequences) pass through the library's workspace under the rules given at nt_conv2d_implicit, and are added in the order
+ * of the keys; without room for them every sequence's keys are one program's. */
 nt_status nt_sdpa_paged_tree(const void *q, const nt_tensor_desc *dq, const nt_paged_cache *cache, const int32_t *table, const nt_tensor_desc *d_table,
                              const int32_t *starts, const int32_t *lengths, const uint64_t *masks, const nt_tensor_desc *d_masks, const int32_t *depths,
                              void *out, const nt_tensor_desc *dout, float scale, int64_t window, int64_t max_queries, int64_t max_length, nt_dtype dtype, void *hip_stream);
@@ -449,8 +454,8 @@ nt_status nt_cache_compact(const nt_paged_cache *caches, int64_t n_caches, const
 
 /* How the calling thread's last nt_sdpa_paged or nt_sdpa_paged_tree call was laid out; zeros if nothing was launched.  For tests and diagnostics. */
 typedef struct {
-    int32_t rows;            /* (token, query head) rows per program: 16 or 32 (wavefronts share the keys), or 128 (they share the rows) */
-    int32_t shares;          /* programs that a row's keys are shared out over */
+    int32_t rows;            /* (token, query head) rows per program: 16 or 32 (wavefronts share the keys), or 128 (they share the rows); trees: 64 or 128 */
+    int32_t shares;          /* programs that a row's keys are shared out over (trees: that all sequences' keys are) */
     int32_t share_keys;      /* keys of one share (0: not shared) */
 } nt_paged_plan;
 nt_status nt_last_paged_plan(nt_paged_plan *out);

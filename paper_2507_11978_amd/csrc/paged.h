@@ -116,6 +116,33 @@ __device__ __forceinline__ uint32_t rest_of(uint32_t packed, float a, float b)
     return pack_two<BF16>(x, y);
 }
 
+// Two weights as the sums of two 16-bit numbers each, the first cut off, so that the rest is not negative: as long as it is more than 0 an infinity that it multiplies stays
+// one, which the rest of a rounded weight, of either sign or 0, makes NaN.  A rest of 0 becomes the type's smallest normal number (fp16: smallest of all, 2^-24 of a weight of 1);
+// that of a weight of 0 stays 0.  Off by 2^-16 of the weight in bf16, 2^-22 or 2^-24 of a weight of 1 in fp16.  SCALED: as above; values then are codes, no infinities.
+template <bool BF16, bool SCALED>
+__device__ __forceinline__ void cut_two(float a, float b, uint32_t *first, uint32_t *rest)
+{
+    float x, y;
+    if constexpr (BF16) {
+        *first = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, a), 0x07060302u);
+        x = a - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, a) & 0xffff0000u);
+        y = b - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, b) & 0xffff0000u);
+    } else {
+        *first = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
+        x = a - widen_one<false>(*first, 0);
+        y = b - widen_one<false>(*first, 1);
+    }
+    if constexpr (SCALED) {
+        x = __builtin_fabsf(x) < INFINITY ? x : 0.f;
+        y = __builtin_fabsf(y) < INFINITY ? y : 0.f;
+    } else {
+        constexpr float least = BF16 ? 0x1p-126f : 0x1p-24f;
+        x = __builtin_amdgcn_fmed3f(x, a, least);
+        y = __builtin_amdgcn_fmed3f(y, b, least);
+    }
+    *rest = pack_two<BF16>(x, y);
+}
+
 // v if it is an infinity or NaN, else 0
 __device__ __forceinline__ float only_not_finite(float v) { return __builtin_fabsf(v) < INFINITY ? 0.f : v; }
 
@@ -197,6 +224,9 @@ struct PagedArgs {
     const int32_t *depths;
     int64_t m_st;
     int32_t words;
+    int32_t parts;                     // programs that a sequence's rows are dealt out to,
+    int32_t groups;                    // ... and that all sequences' keys are dealt out to (0: each sequence and head has one)
+    int64_t *before;                   // blocks of the sequences before each, and of all
     float scale_log2e;                 // scale * log2(e): exponentials are taken in base 2
     // one program's share of a row (splits > 1): [token * Hq + head][split] of (reference, sum), and of D unnormalised outputs
     float *part_ml, *part_o;
@@ -207,11 +237,6 @@ __device__ __forceinline__ Sequence sequence_of(const PagedArgs &g, int b) { ret
 __device__ __forceinline__ KeyRange keys_of(const PagedArgs &g, const Sequence &q, int32_t i0, int32_t i1, int split, int32_t block)
 {
     return key_range(q, i0, i1, g.causal, g.window, split, g.splits, g.split_keys, block, g.width * (int32_t)g.page.d);
-}
-
-__device__ __forceinline__ KeyRange tree_keys_of(const PagedArgs &g, const Sequence &q, int split, int32_t block)
-{
-    return tree_range(q, g.window, split, g.splits, g.split_keys, block, g.width * (int32_t)g.page.d);
 }
 
 // ---- where a block of keys lies in LDS: rows of SIZE 16-bit elements, their 16-byte chunks in an order that depends on the row, such that 16
@@ -239,6 +264,9 @@ constexpr uint32_t kNanPair = 0x7fff7fffu;
 nt_status launch_paged_64(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream);
 nt_status launch_paged_128(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream);
 nt_status launch_paged_256(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream);
+// sequences whose keys the tree kernel deals out evenly
+constexpr int kTreeSequences = 1024;
+
 nt_status launch_paged_tree_64(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream);
 nt_status launch_paged_tree_128(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream);
 nt_status launch_paged_tree_256(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream);

@@ -3,6 +3,6 @@
 
 namespace nt {
 
-nt_status launch_paged_128(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream) { return launch_paged_size<128, false>(a, rows, programs, bf16, kind, stream); }
+nt_status launch_paged_128(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream) { return launch_paged_size<128>(a, rows, programs, bf16, kind, stream); }
 
 }  // namespace nt

@@ -3,6 +3,6 @@
 
 namespace nt {
 
-nt_status launch_paged_256(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream) { return launch_paged_size<256, false>(a, rows, programs, bf16, kind, stream); }
+nt_status launch_paged_256(const PagedArgs &a, int rows, int64_t programs, bool bf16, int kind, void *stream) { return launch_paged_size<256>(a, rows, programs, bf16, kind, stream); }
 
 }  // namespace nt

@@ -109,6 +109,34 @@ static void launch_join(const PagedArgs &a, hipStream_t s)
 static thread_local nt_paged_plan t_paged;
 const nt_paged_plan &last_paged_plan() { return t_paged; }
 
+static nt_status launch_tree(PagedArgs &a, int64_t group_rows, int built, bool bf16, int kind, void *stream)
+{
+    const int rows = group_rows <= kManyRows / 2 && built < 256 ? kManyRows / 2 : kManyRows;
+    // (without a bound on the new tokens: twice their mean)
+    const int64_t mean = 2 * ((int64_t)a.T / a.B + 1) * a.G, parts = (std::min(group_rows, mean) + rows - 1) / rows;
+    const int64_t inner = a.Hkv * parts;
+    int64_t groups = std::max<int64_t>(1, (built == 256 ? 256 : 512) / inner), programs = groups * inner;
+    WorkspaceLease lease;
+    char *ws = nullptr;
+    const size_t n = (size_t)(2 * programs * rows), room = (size_t)(kTreeSequences + 8) * 8;
+    if (a.B <= kTreeSequences) ws = (char *)lease.acquire(room + n * (size_t)(2 + a.D) * 4, (hipStream_t)stream);
+    if (ws) {
+        a.before = (int64_t *)ws;
+        a.part_ml = (float *)(ws + room);
+        a.part_o = a.part_ml + 2 * n;
+    } else {
+        groups = 0;
+        programs = (int64_t)a.B * a.Hkv * parts;
+    }
+    if (programs > kMaxWorkgroups || (int64_t)a.B * a.Hkv * parts > kMaxWorkgroups) return fail(NT_ERR_UNSUPPORTED, "too many programs for one launch");
+    a.groups = (int32_t)groups;
+    a.parts = (int32_t)parts;
+    auto launch = built == 64 ? launch_paged_tree_64 : built == 128 ? launch_paged_tree_128 : launch_paged_tree_256;
+    const nt_status st = launch(a, rows, programs, bf16, kind, stream);
+    if (st == NT_OK) t_paged = nt_paged_plan{rows, (int32_t)std::max<int64_t>(1, groups), 0};
+    return st;
+}
+
 nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_paged_cache *c, const int32_t *table, const nt_tensor_desc *dt,
                             const int32_t *starts, const int32_t *lengths, void *out, const nt_tensor_desc *dout,
                             float scale, int causal, int64_t window, int64_t max_queries, int64_t max_length, int dtype, void *stream, const TreeMasks *tree)
@@ -182,6 +210,7 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     // keys 14.0, by the other 27.4, 1 x 8000 18.5 / 25.5, 32 x 2000 57.7 / 81.0; 4 x 16 heads x 64 f16, 8000 35.3 / 42.1).
     const int64_t most = max_queries && max_queries < T ? max_queries : T, group_rows = most * a.G;
     const int built = D <= 64 ? 64 : D <= 128 ? 128 : 256;
+    if (tree) return launch_tree(a, group_rows, built, dtype == NT_BF16, kind, stream);
     const int rows = group_rows <= 16 ? 16 : group_rows <= 32 && built < 256 ? 32 : kManyRows;
     a.tiles = rows == kManyRows ? (int32_t)(T * a.G / kManyRows + B) : (int32_t)B;
     const int64_t base = (int64_t)a.tiles * Hkv;
@@ -220,8 +249,7 @@ nt_status launch_sdpa_paged(const void *q, const nt_tensor_desc *dq, const nt_pa
     a.splits = (int32_t)splits;
     a.split_keys = (int32_t)std::min<int64_t>(share, 0x7fffffff / 2);
     const bool bf16 = dtype == NT_BF16;
-    auto launch = built == 64 ? (tree ? launch_paged_tree_64 : launch_paged_64) : built == 128 ? (tree ? launch_paged_tree_128 : launch_paged_128)
-                                                                                          : (tree ? launch_paged_tree_256 : launch_paged_256);
+    auto launch = built == 64 ? launch_paged_64 : built == 128 ? launch_paged_128 : launch_paged_256;
     nt_status rc = launch(a, rows, base * splits, bf16, kind, stream);
     if (rc != NT_OK) return rc;
     if (splits > 1) {

@@ -35,8 +35,7 @@ constexpr int few_resident(int size, int mb) { return mb == 1 && size == 64 ? 3 
 
 // UNIFORM: page_size is a multiple of 16, so that 16 keys that begin at a multiple of 16 lie on one page: the table is read and the addresses are made
 // once for a wavefront, on the scalar unit, and a lane's part is an offset that never changes.
-// TREE: the new tokens are a tree's, what a row sees of them stands in its mask; [row_lo, row_hi) is what it sees of the past.
-template <bool BF16, int KIND, int SIZE, int MB, bool UNIFORM, bool FULL, bool TREE>
+template <bool BF16, int KIND, int SIZE, int MB, bool UNIFORM, bool FULL>
 __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_few_kernel(const PagedArgs g)
 {
     constexpr int KS = SIZE / 32;                                          // k steps of the first product
@@ -142,29 +141,20 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
 
     for (int r0 = 0; r0 < rows_all; r0 += 16 * MB) {                       // (one pass, unless the caller's bound on new tokens was too low)
         const int last = r0 + 16 * MB < rows_all ? r0 + 16 * MB - 1 : rows_all - 1;
-        const KeyRange keys = TREE ? tree_keys_of(g, seq, split, TRIP) : keys_of(g, seq, (int32_t)divide(r0, g.group), (int32_t)divide(last, g.group), split, TRIP);
+        const KeyRange keys = keys_of(g, seq, (int32_t)divide(r0, g.group), (int32_t)divide(last, g.group), split, TRIP);
 
         const int t_end = keys.lo < keys.hi ? (keys.hi + TRIP - 1) / TRIP : 0;
         int t = keys.lo / TRIP + wave;
 
         // ---- this lane's rows (row c16 of each 16): their keys [row_lo, row_hi), and Q as the first product's operand
         int32_t row_lo[MB], row_hi[MB];
-        const uint64_t *mask[TREE ? MB : 1];
         u32x4 qf[MB][KS];
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
             const int r = r0 + 16 * mb + c16;
             const bool real = r < rows_all;
             const uint32_t rc = real ? r : last, i = divide(rc, g.group), head = h * g.G + (rc - i * g.group.d);
-            KeyRange sees;
-            if constexpr (TREE) {
-                const int64_t token = seq.first + (int32_t)i;
-                const int32_t past = seq.length - seq.count;
-                sees = KeyRange{tree_row_lo(past, seq.count, g.window ? g.depths[token] : 0, g.window), past};
-                mask[mb] = g.masks + token * g.m_st;
-            } else {
-                sees = keys_seen(seq, (int32_t)i, g.causal, g.window);
-            }
+            const KeyRange sees = keys_seen(seq, (int32_t)i, g.causal, g.window);
             row_lo[mb] = real ? sees.lo : INT32_MIN;                       // (rows past the last are not stored: nothing to hide from them)
             row_hi[mb] = real ? sees.hi : INT32_MAX;
             const uint16_t *q = g.Q + (int64_t)(seq.first + (int32_t)i) * g.q_st + (int64_t)head * g.q_sh;
@@ -264,18 +254,6 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
 #pragma unroll
             for (int mb = 0; mb < MB; ++mb) clear = clear && row_lo[mb] <= base && base + TRIP <= row_hi[mb];
             clear = __all(clear);
-            uint64_t vis[TREE ? MB : 1];                                    // which keys of the trip the row sees
-            auto sees = [&](int mb, int32_t key) {
-                if constexpr (TREE) return ((vis[mb] >> (key - base)) & 1) != 0;
-                else return key >= row_lo[mb] && key < row_hi[mb];
-            };
-            if constexpr (TREE) {
-#pragma unroll
-                for (int mb = 0; mb < MB; ++mb) {
-                    vis[mb] = ~0ull;
-                    if (!clear && row_hi[mb] != INT32_MAX) vis[mb] = tree_keys(mask[mb], g.words, base, row_lo[mb], row_hi[mb], seq.length);
-                }
-            }
             bool careful = false;                                          // (codes: some row does not see a NaN)
             if (all != 0xffffu || !clear) {                                // wavefront-uniform
                 bool odd = false;
@@ -319,7 +297,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
                         for (int v = 0; v < 4; ++v) {
                             const int32_t key = base + 16 * u + q + v;
                             const float x = (named[u] >> (q + v)) & 1 ? s[4 * u + v] : __builtin_nanf("");
-                            s[4 * u + v] = sees(mb, key) ? x : -INFINITY;        // (shares begin and end between trips)
+                            s[4 * u + v] = key >= row_lo[mb] && key < row_hi[mb] ? x : -INFINITY;        // (shares begin and end between trips)
                         }
                 }
                 float top = s[0];
@@ -352,7 +330,7 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
 #pragma unroll
                         for (int j = 0; j < 4 * NG; ++j) {
                             const int32_t key = first + 16 * (j / 4) + j % 4;
-                            p[j] = sees(mb, key) ? p[j] : 0.f;
+                            p[j] = key >= row_lo[mb] && key < row_hi[mb] ? p[j] : 0.f;
                         }
                     }
                 }
@@ -403,11 +381,11 @@ __global__ __launch_bounds__(64 * kFewWaves, few_resident(SIZE, MB)) void paged_
                             const int32_t key = base + 32 * i + j;
 #pragma unroll
                             for (int mb = 0; mb < MB; ++mb) {
-                                const bool seen = sees(mb, key);
+                                const bool sees = key >= row_lo[mb] && key < row_hi[mb];
 #pragma unroll
                                 for (int e = 0; e < 4; ++e) {
                                     const float x = only_not_finite(widen_one<VB>(v[e >> 1], e & 1));
-                                    acc[mb][db][e] += seen ? x : 0.f;
+                                    acc[mb][db][e] += sees ? x : 0.f;
                                 }
                             }
                         }

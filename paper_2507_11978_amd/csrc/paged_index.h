@@ -108,18 +108,28 @@ NT_HD uint64_t tree_keys(const uint64_t *mask, int32_t words, int32_t base, int3
     return before | (bits_from(mask, words, -first) & bits_between(first, end));
 }
 
-// The keys that a program of a tree's rows walks: all that some token may see, or share number `split` of them (as key_range).  Where the past passes what the table
-// reaches, whoever sees anything sees a position without a page among the last of the past and the new ones: no others are needed to show it.
-NT_HD KeyRange tree_range(const Sequence &q, int32_t window, int split, int splits, int32_t share_keys, int32_t block, int32_t capacity)
+// The keys that some token of a tree may see.  Where the past passes what the table reaches, whoever sees anything sees a position without a page among the last of the past and
+// the new ones: no others are needed to show it.
+NT_HD KeyRange tree_range(const Sequence &q, int32_t window, int32_t capacity)
 {
     const int32_t past = q.length - q.count;
-    int32_t lo = past > capacity ? past - 1 : window && past >= window ? past - window + 1 : 0, hi = q.length;
-    if (splits > 1) {
-        const int64_t base = lo / block * block, from = base + (int64_t)split * share_keys, to = from + share_keys;
-        if (split > 0 && from > lo) lo = from > hi ? hi : (int32_t)from;
-        if (split + 1 < splits && to < hi) hi = (int32_t)to;
-    }
-    return KeyRange{lo, hi < lo ? lo : hi};
+    return KeyRange{past > capacity ? past - 1 : window && past >= window ? past - window + 1 : 0, q.length};
+}
+
+// ... in blocks of `block` keys; tokens that see nothing have a block too
+NT_HD int32_t tree_blocks(const Sequence &q, int32_t window, int32_t block, int32_t capacity)
+{
+    if (q.count == 0) return 0;
+    const KeyRange k = tree_range(q, window, capacity);
+    const int32_t n = k.lo < k.hi ? (k.hi - 1) / block + 1 - k.lo / block : 0;
+    return n > 0 ? n : 1;
+}
+
+// Blocks [from, to) of it
+NT_HD KeyRange tree_part(const KeyRange &k, int32_t block, int32_t blocks, int32_t from, int32_t to)
+{
+    const int32_t first = k.lo / block;
+    return KeyRange{from ? (first + from) * block : k.lo, to < blocks ? (first + to) * block : k.hi};
 }
 
 // The page of a position, in two steps: its entry of the table row is on its way long before the page is needed.

@@ -41,9 +41,12 @@ constexpr size_t many_lds(int size) { return 4 * many_block(size) + 2 * 2 * many
 constexpr int many_resident(int kind, int size) { return size == 256 ? 1 : size == 128 || kind != CACHE_SAME ? 2 : 3; }
 
 // FULL: rows of SIZE elements (the switched-off lanes of others cost 5 % where none is: 1024 queries x 8000 keys x 32/8 heads x 128 bf16 217 us, 228)
-// TREE: as in paged_few.h
-template <bool BF16, int KIND, int SIZE, bool FAST, bool FULL, bool TREE>
-__global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void paged_many_kernel(const PagedArgs g)
+// One tile: the rows of a sequence and key head from r0 on.
+// TREE: the new tokens are a tree's, what a row sees of them stands in its mask; [row_lo, row_hi) is what it sees of the past.  The tile's keys are given, and where its share of the
+// result goes, if it is one.  Weights multiply V as the sum of two 16-bit numbers (cut_two).  GROUPS: of wavefronts that share a block's keys, the rows being fewer by so much.
+template <bool BF16, int KIND, int SIZE, bool FAST, bool FULL, bool TREE, int GROUPS>
+__device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const smem, const int b, const int h, const Sequence &seq, const int r0,
+                                                const int split, const KeyRange given, float *const share_ml, float *const share_o)
 {
     constexpr bool DMA = FAST && KIND == CACHE_SAME;
     constexpr int EPL = FAST ? many_piece(KIND) : 8;
@@ -51,46 +54,30 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
     constexpr int ES = KIND == CACHE_SAME ? 2 : 1;
     constexpr uint32_t BLK = many_block(SIZE);
     constexpr bool VB = BF16 || KIND != CACHE_SAME;                        // the second product's type is bf16,
-    constexpr bool SPLIT = VB && !BF16;                                    // ... where that is not the queries', with weights in two parts: see rest_of
+    constexpr bool SPLIT = TREE || (VB && !BF16);                          // ... where that is not the queries', with weights in two parts: see rest_of
+    constexpr bool SUMS = TREE || KIND != CACHE_SAME;                      // sums of the weights as they are, each lane of its keys
+    constexpr int ROWS = kManyRows / GROUPS, ROW_WAVES = kManyWaves / GROUPS, JW = JB / GROUPS;     // 32-key parts of a block to a wavefront
+    static_assert(GROUPS == 1 || TREE, "built");
     constexpr int DEEP = 4;                                                // products that a fragment of K or V is read ahead of its own
-    extern __shared__ __attribute__((aligned(1024))) char smem[];
     float *const scales = reinterpret_cast<float *>(smem + 4 * BLK);
     int *const flags = reinterpret_cast<int *>(scales + 4 * KB);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, hi = lane >> 5;
 
-    // ---- which tile: head fastest (a head's tiles on one XCD, where the heads are a multiple of 8), then share, then tile, the sequences' last first: they
-    // see the most keys.
-    int w = blockIdx.x;
-    const int h = w % g.Hkv;
-    w /= g.Hkv;
-    const int split = w % g.splits, number = g.tiles - 1 - w / g.splits;
-    auto tiles_before = [&](int b) { return first_tile(g.starts, b, g.T, g.G, kManyRows); };
-    int b = 0;
-    for (int up = g.B; up - b > 1;) {                                      // 64 sequences at a time: the last whose tiles begin at or before this one
-        const int step = (up - b + 63) / 64, at = b + lane * step;
-        const uint64_t below = __ballot(at < up && tiles_before(at < up ? at : b) <= number);
-        const int found = below ? 63 - __builtin_clzll(below) : 0;
-        b += found * step;
-        up = b + step < up ? b + step : up;
-    }
-    const Sequence seq = sequence_of(g, b);
-    const int64_t r0_64 = (int64_t)(number - tiles_before(b)) * kManyRows;
-    const int rows_all = seq.count * g.G;
-    if (r0_64 < 0 || r0_64 >= rows_all) return;                            // (workgroup-uniform)
-    const int r0 = (int)r0_64, tile_last = r0 + kManyRows < rows_all ? r0 + kManyRows - 1 : rows_all - 1;
+    const int rows_all = seq.count * g.G, tile_last = r0 + ROWS < rows_all ? r0 + ROWS - 1 : rows_all - 1;
     const int32_t *pages = g.table + (int64_t)b * g.t_sb;
     const char *Kh = g.K + (int64_t)h * g.k_sh * ES, *Vh = g.V + (int64_t)h * g.v_sh * ES;
     const int32_t tile_i0 = (int32_t)divide(r0, g.group), tile_i1 = (int32_t)divide(tile_last, g.group);
-    const KeyRange keys = TREE ? tree_keys_of(g, seq, split, KB) : keys_of(g, seq, tile_i0, tile_i1, split, KB);
+    const KeyRange keys = TREE ? given : keys_of(g, seq, tile_i0, tile_i1, split, KB);
     // keys that every row of the tile sees: [seen_lo, seen_hi) (a tree's rows: no token is deeper than their count)
     const int32_t past = seq.length - seq.count;
     const int32_t seen_lo = TREE ? tree_row_lo(past, seq.count, seq.count, g.window) : keys_seen(seq, tile_i1, g.causal, g.window).lo;
     const int32_t seen_hi = TREE ? past : keys_seen(seq, tile_i0, g.causal, g.window).hi;
 
     // ---- this lane's row and its keys [row_lo, row_hi); the wavefront's: seen by some row [wave_lo, wave_hi), by all [all_lo, all_hi)
-    const int row = r0 + 32 * wave + l32;
+    const int row_wave = wave % ROW_WAVES, jw = wave / ROW_WAVES * JW;     // the wavefront's part of a block: 32-key parts from number jw on
+    const int row = r0 + 32 * row_wave + l32;
     const bool real = row < rows_all;
-    const bool busy = r0 + 32 * wave < rows_all;                           // wavefront-uniform
+    const bool busy = r0 + 32 * row_wave < rows_all;                       // wavefront-uniform
     const uint32_t rc = real ? row : tile_last, mine = divide(rc, g.group), head = h * g.G + (rc - mine * g.group.d);
     const int64_t token = seq.first + (int32_t)mine;
     const KeyRange row_keys = TREE ? KeyRange{tree_row_lo(past, seq.count, g.window ? g.depths[token] : 0, g.window), past} : keys_seen(seq, (int32_t)mine, g.causal, g.window);
@@ -254,56 +241,58 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
     for (int db = 0; db < SIZE / 32; ++db)
 #pragma unroll
         for (int v = 0; v < 16; ++v) ot[db][v] = 0.f;
-    float m_ref = -INFINITY, l_run = 0.f;                                  // reference (-inf: none yet) and sum (8-bit caches: of this lane's keys)
+    float m_ref = -INFINITY, l_run = 0.f;                                  // reference (-inf: none yet) and sum (SUMS: of this lane's keys)
     bool pending = true;                                                   // wavefront-uniform: some row has no reference
     const uint32_t one_pair = ((lane >> 4) & 1) == ((lane >> 2) & 1) ? (BF16 ? 0x3f803f80u : 0x3c003c00u) : 0u;
     const u32x4 ones{one_pair, one_pair, one_pair, one_pair};              // (the sum of query lane % 32 in every lane: see attention.hip)
     const int gq = lane >> 4, li = lane & 15;
     const uint32_t v_key = 4 * (gq >> 1) + (li >> 2), v_chunk = 2 * (gq & 1) + ((li >> 1) & 1), v_half = (li & 1) * 8;
 
-    u32x4 pk[JB][2];                                                       // a block's weights, packed (8-bit caches: times the values' scales)
-    u32x4 rest[SPLIT ? JB : 1][2];                                         // ... and what their rounding left
+    u32x4 pk[JW][2];                                                       // a block's weights, packed (8-bit caches: times the values' scales)
+    u32x4 rest[SPLIT ? JW : 1][2];                                         // ... and what their rounding left
     auto weigh = [&](const int kb, const uint32_t copy) __attribute__((always_inline)) {
         const int base = kb * KB;
         const char *ks_lds = smem + copy * BLK;
         // ---- S^T: st[jb][v] <-> key 32 jb + 8 (v / 4) + 4 hi + v % 4, query l32
-        float16v st[JB];
+        float16v st[JW];
 #pragma unroll
-        for (int jb = 0; jb < JB; ++jb)
+        for (int jb = 0; jb < JW; ++jb)
 #pragma unroll
             for (int v = 0; v < 16; ++v) st[jb][v] = 0.f;
         // (product by product, in an order that is pinned: left to itself the compiler reads a fragment when it is due and waits for it, 666 us against 643
         // for 2048 queries of 32 heads over 18500 keys; DEEP 6: 642)
-        constexpr int PRODUCTS = SIZE / 16 * JB;
-        auto fragment = [&](int i) __attribute__((always_inline)) { return lds_read16(ks_lds, lds_at<SIZE>(32 * (i % JB) + l32, 2 * (i / JB) + hi)); };
+        constexpr int PRODUCTS = SIZE / 16 * JW;
+        auto fragment = [&](int i) __attribute__((always_inline)) {
+            return lds_read16(ks_lds + (GROUPS > 1 ? jw * 64 * SIZE : 0), lds_at<SIZE>(32 * (i % JW) + l32, 2 * (i / JW) + hi));
+        };
         u32x4 f[DEEP];
 #pragma unroll
         for (int i = 0; i < DEEP; ++i) f[i] = fragment(i);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < PRODUCTS; ++i) {
-            st[i % JB] = mfma32<BF16>(f[i % DEEP], qf[i / JB], st[i % JB]);
+            st[i % JW] = mfma32<BF16>(f[i % DEEP], qf[i / JW], st[i % JW]);
             if (i + DEEP < PRODUCTS) f[i % DEEP] = fragment(i + DEEP);
             __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (KIND != CACHE_SAME) {
 #pragma unroll
-            for (int jb = 0; jb < JB; ++jb)
+            for (int jb = 0; jb < JW; ++jb)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const float4v k4 = *reinterpret_cast<const float4v *>(&scales[copy * 2 * KB + 32 * jb + 8 * q + 4 * hi]);
+                    const float4v k4 = *reinterpret_cast<const float4v *>(&scales[copy * 2 * KB + 32 * (GROUPS > 1 ? jw + jb : jb) + 8 * q + 4 * hi]);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) st[jb][4 * q + e] *= k4[e];
                 }
         }
         const bool hidden = base < all_lo || base + KB > all_hi;          // wavefront-uniform: from some row
-        uint64_t vis = ~0ull;                                              // (TREE: which keys of the block the row sees, from key 4 hi on)
+        uint64_t vis = ~0ull;                                              // (TREE: which keys of the wavefront's part of the block the row sees, from key 4 hi on)
         if constexpr (TREE) {
             if (hidden) {
                 const float out = g.scale_log2e >= 0.f ? -INFINITY : INFINITY;
-                vis = row_bits(base) >> (4 * hi);
+                vis = row_bits(base + 32 * jw) >> (4 * hi);
 #pragma unroll
-                for (int jb = 0; jb < JB; ++jb)
+                for (int jb = 0; jb < JW; ++jb)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) st[jb][v] = (vis >> (32 * jb + 8 * (v / 4) + v % 4)) & 1 ? st[jb][v] : out;
             }
@@ -311,7 +300,7 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
             const float out = g.scale_log2e >= 0.f ? -INFINITY : INFINITY;
             const uint32_t from = here(base + 4 * hi) - row_lo, count = row_hi > row_lo ? row_hi - row_lo : 0;      // (keys before row_lo: far beyond count)
 #pragma unroll
-            for (int jb = 0; jb < JB; ++jb)
+            for (int jb = 0; jb < JW; ++jb)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) st[jb][v] = from + (uint32_t)(32 * jb + 8 * (v / 4) + v % 4) < count ? st[jb][v] : out;
         }
@@ -320,7 +309,7 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
         auto exponentials = [&](const float m) {
             float sum = 0.f;
 #pragma unroll
-            for (int jb = 0; jb < JB; ++jb)
+            for (int jb = 0; jb < JW; ++jb)
 #pragma unroll
                 for (int s2 = 0; s2 < 2; ++s2)
 #pragma unroll
@@ -328,20 +317,26 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
                         float p[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[jb][8 * s2 + 4 * q + e], g.scale_log2e, -m));
+                        if constexpr (SUMS) sum += (p[0] + p[1]) + (p[2] + p[3]);
                         if constexpr (KIND != CACHE_SAME) {
-                            sum += (p[0] + p[1]) + (p[2] + p[3]);
-                            const float4v v4 = *reinterpret_cast<const float4v *>(&scales[copy * 2 * KB + KB + 32 * jb + 16 * s2 + 8 * q + 4 * hi]);
+                            const float4v v4 = *reinterpret_cast<const float4v *>(&scales[copy * 2 * KB + KB + 32 * (GROUPS > 1 ? jw + jb : jb) + 16 * s2 + 8 * q + 4 * hi]);
 #pragma unroll
                             for (int e = 0; e < 4; ++e) p[e] *= v4[e];
                         }
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            const uint32_t w = pack_two<VB>(p[2 * i], p[2 * i + 1]);
+                            uint32_t w, r = 0;
+                            if constexpr (TREE) {
+                                cut_two<VB, KIND != CACHE_SAME>(p[2 * i], p[2 * i + 1], &w, &r);
+                            } else {
+                                w = pack_two<VB>(p[2 * i], p[2 * i + 1]);
+                                if constexpr (SPLIT) r = rest_of<VB, true>(w, p[2 * i], p[2 * i + 1]);
+                            }
                             pk[jb][s2][2 * q + i] = w;
-                            if constexpr (SPLIT) rest[jb][s2][2 * q + i] = rest_of<VB, true>(w, p[2 * i], p[2 * i + 1]);
+                            if constexpr (SPLIT) rest[jb][s2][2 * q + i] = r;
                         }
                     }
-            if constexpr (KIND != CACHE_SAME) rs = sum;
+            if constexpr (SUMS) rs = sum;
         };
         // the sums of the packed weights on the matrix pipe; `apart`: queries 0 .. 15 and 16 .. 31 by instructions of their own (0 * NaN is NaN: what
         // one holds would reach the other; the sums are the same bits either way)
@@ -351,7 +346,7 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
             for (int half = 0; half < 2; ++half) {
                 if (half && !apart) break;
 #pragma unroll
-                for (int jb = 0; jb < JB; ++jb)
+                for (int jb = 0; jb < JW; ++jb)
 #pragma unroll
                     for (int s2 = 0; s2 < 2; ++s2)
                         sum[half] = mfma16<BF16>(ones, !apart || (l32 >> 4) == half ? pk[jb][s2] : u32x4{0, 0, 0, 0}, sum[half]);
@@ -362,30 +357,30 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
         bool accept = false;
         if (!pending) {
             exponentials(m_ref);
-            if constexpr (KIND == CACHE_SAME) rs = matrix_sum(false);
+            if constexpr (!SUMS) rs = matrix_sum(false);
             accept = __all(rs < 32768.f);
         }
         if (!accept) {                                                     // wavefront-uniform: a row without reference, or a score far above M
             bool keep = false;                                             // this row's reference is close enough
             if (__any(m_ref != -INFINITY)) {
                 exponentials(m_ref == -INFINITY ? 0.f : m_ref);
-                if constexpr (KIND == CACHE_SAME) rs = matrix_sum(true);
+                if constexpr (!SUMS) rs = matrix_sum(true);
                 keep = m_ref != -INFINITY && rs < 32768.f;
-                if constexpr (KIND != CACHE_SAME) {
+                if constexpr (SUMS) {
                     const float other = __shfl_xor(rs, 32, 64);            // the row's other lane (exchanged by all: a lane that is switched off reads as 0)
                     keep = keep && other < 32768.f;
                 }
             }
             float mx = -INFINITY;
 #pragma unroll
-            for (int jb = 0; jb < JB; ++jb)
+            for (int jb = 0; jb < JW; ++jb)
 #pragma unroll
                 for (int v = 0; v < 16; ++v) mx = fmaxf(mx, st[jb][v] * g.scale_log2e);
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
             const float m_new = keep ? m_ref : fmaxf(m_ref, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
             const float alpha = __builtin_amdgcn_exp2f(m_ref - m_use);
             exponentials(m_use);
-            if constexpr (KIND == CACHE_SAME) rs = matrix_sum(true);
+            if constexpr (!SUMS) rs = matrix_sum(true);
             l_run *= alpha;
 #pragma unroll
             for (int db = 0; db < SIZE / 32; ++db)
@@ -398,7 +393,7 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
         if constexpr (TREE && KIND != CACHE_SAME) {
             if (hidden) {
 #pragma unroll
-                for (int i = 0; i < 8 * JB; ++i) {
+                for (int i = 0; i < 8 * JW; ++i) {
                     const uint32_t two = (uint32_t)(vis >> (8 * (i / 2) + 2 * (i % 2))) & 3, seen = (two & 1 ? 0xffffu : 0u) | (two & 2 ? 0xffff0000u : 0u);
                     pk[i / 8][i / 4 % 2][i % 4] &= seen;
                     if constexpr (SPLIT) rest[i / 8][i / 4 % 2][i % 4] &= seen;
@@ -407,7 +402,7 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
         } else if (KIND != CACHE_SAME && hidden) {                         // (the scale of a hidden key may be anything; a seen one's NaN shows whatever its weight)
             const uint32_t from = here(base + 4 * hi) - row_lo, count = row_hi > row_lo ? row_hi - row_lo : 0;
 #pragma unroll
-            for (int i = 0; i < 8 * JB; ++i) {                             // pair i: key 8 (i / 2) + 4 hi + 2 (i % 2) of the block and the next
+            for (int i = 0; i < 8 * JW; ++i) {                             // pair i: key 8 (i / 2) + 4 hi + 2 (i % 2) of the block and the next
                 const uint32_t j = from + (uint32_t)(8 * (i / 2) + 2 * (i % 2));
                 const uint32_t seen = (j < count ? 0xffffu : 0u) | (j + 1 < count ? 0xffff0000u : 0u);
                 pk[i / 8][i / 4 % 2][i % 4] &= seen;
@@ -418,7 +413,8 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
     // ---- O^T += V^T P^T: k step (jb, s2) lists its 16 keys as 32 jb + 16 s2 + 8 part + 4 hi + 0 .. 3
     auto add_values = [&](const uint32_t copy) __attribute__((always_inline)) {
         const char *vs_lds = smem + (2 + copy) * BLK;
-        constexpr int DB = SIZE / 32, PRODUCTS = 2 * JB * DB;
+        constexpr int DB = SIZE / 32, PRODUCTS = 2 * JW * DB;
+        if constexpr (GROUPS > 1) vs_lds += jw * 64 * SIZE;
         auto fragment = [&](int i) __attribute__((always_inline)) {
             const int key = 16 * (i / DB), chunk = 4 * (i % DB);
             const u32x2 a = lds_read_transposed(vs_lds, lds_at<SIZE>(key + v_key, chunk + v_chunk) + v_half);
@@ -441,10 +437,10 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
     auto add_not_finite = [&](const int kb, const uint32_t copy) {
         const char *vs_lds = smem + (2 + copy) * BLK;
         const int half = here(hi);
-        const uint64_t vis = TREE ? row_bits(kb * KB) : 0;
+        const uint64_t vis = TREE ? row_bits(kb * KB + 32 * jw) : 0;
 #pragma unroll 1
-        for (int j = 0; j < KB; ++j) {
-            const bool sees = TREE ? (vis >> j) & 1 : kb * KB + j >= row_lo && kb * KB + j < row_hi;
+        for (int j = 32 * jw; j < 32 * (jw + JW); ++j) {
+            const bool sees = TREE ? (vis >> (j - 32 * jw)) & 1 : kb * KB + j >= row_lo && kb * KB + j < row_hi;
 #pragma unroll
             for (int db = 0; db < SIZE / 32; ++db)
 #pragma unroll
@@ -500,10 +496,31 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
     }
 
     // ---- O = O^T / l, stored along d: after the half-wavefronts trade register groups a lane owns d = 32 db + 16 hi .. + 15 of its row
-    const float total = KIND == CACHE_SAME ? l_run : l_run + __shfl_xor(l_run, 32, 64);
-    const float factor = g.splits > 1 ? 1.f : total == 0.f ? 0.f : 1.0f / total;
-    const int64_t at = (token * g.Hq + head) * g.splits + split;
-    if (g.splits > 1 && real && hi == 0) *reinterpret_cast<float2v *>(g.part_ml + 2 * at) = float2v{m_ref, total};
+    float total = SUMS ? l_run + __shfl_xor(l_run, 32, 64) : l_run;
+    if constexpr (GROUPS > 1) {
+        // the other group's results, lane by lane through LDS, to a common maximum
+        static_assert(GROUPS == 2, "two groups");
+        float *ex = reinterpret_cast<float *>(smem) + row_wave * (SIZE / 2 + 2) * 64 + lane;       // (the loop's last barrier is behind all reads of the blocks)
+        if (jw) {
+            ex[0] = m_ref;
+            ex[64] = total;
+#pragma unroll
+            for (int i = 0; i < SIZE / 2; ++i) ex[64 * (i + 2)] = ot[i / 16][i % 16];
+        }
+        __syncthreads();
+        if (jw) return;
+        const float other = ex[0], top = fmaxf(m_ref, other), ref = top == -INFINITY ? 0.f : top;
+        const float mine = __builtin_amdgcn_exp2f(m_ref - ref), theirs = __builtin_amdgcn_exp2f(other - ref);
+        m_ref = top;
+        total = total * mine + ex[64] * theirs;
+#pragma unroll
+        for (int i = 0; i < SIZE / 2; ++i) ot[i / 16][i % 16] = ot[i / 16][i % 16] * mine + ex[64 * (i + 2)] * theirs;
+    }
+    const bool shared = TREE ? share_ml != nullptr : g.splits > 1;
+    const float factor = shared ? 1.f : total == 0.f ? 0.f : 1.0f / total;
+    const int64_t at = TREE ? 32 * row_wave + l32 : (token * g.Hq + head) * g.splits + split;
+    float *const to_ml = TREE ? share_ml : g.part_ml, *const to_o = TREE ? share_o : g.part_o;
+    if (shared && real && hi == 0) *reinterpret_cast<float2v *>(to_ml + 2 * at) = float2v{m_ref, total};
 #pragma unroll
     for (int db = 0; db < SIZE / 32; ++db) {
 #pragma unroll
@@ -512,8 +529,8 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
         gather_row16(ot[db], o);                                           // (all lanes take part)
         const int d = 32 * db + 16 * hi;
         if (!real || d >= g.D) continue;
-        if (g.splits > 1) {
-            float *dst = g.part_o + at * g.D + d;
+        if (shared) {
+            float *dst = to_o + at * g.D + d;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (d + 4 * i < g.D) __builtin_memcpy(dst + 4 * i, &o[4 * i], 16);
@@ -528,6 +545,33 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
             }
         }
     }
+}
+
+template <bool BF16, int KIND, int SIZE, bool FAST, bool FULL>
+__global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void paged_many_kernel(const PagedArgs g)
+{
+    extern __shared__ __attribute__((aligned(1024))) char smem[];
+    // ---- which tile: head fastest (a head's tiles on one XCD, where the heads are a multiple of 8), then share, then tile, the sequences' last first: they
+    // see the most keys.
+    const int lane = threadIdx.x & 63;
+    int w = blockIdx.x;
+    const int h = w % g.Hkv;
+    w /= g.Hkv;
+    const int split = w % g.splits, number = g.tiles - 1 - w / g.splits;
+    auto tiles_before = [&](int b) { return first_tile(g.starts, b, g.T, g.G, kManyRows); };
+    int b = 0;
+    for (int up = g.B; up - b > 1;) {                                      // 64 sequences at a time: the last whose tiles begin at or before this one
+        const int step = (up - b + 63) / 64, at = b + lane * step;
+        const uint64_t below = __ballot(at < up && tiles_before(at < up ? at : b) <= number);
+        const int found = below ? 63 - __builtin_clzll(below) : 0;
+        b += found * step;
+        up = b + step < up ? b + step : up;
+    }
+    const Sequence seq = sequence_of(g, b);
+    const int64_t r0_64 = (int64_t)(number - tiles_before(b)) * kManyRows;
+    const int rows_all = seq.count * g.G;
+    if (r0_64 < 0 || r0_64 >= rows_all) return;                            // (workgroup-uniform)
+    paged_many_tile<BF16, KIND, SIZE, FAST, FULL, false, 1>(g, smem, b, h, seq, (int)r0_64, split, KeyRange{0, 0}, nullptr, nullptr);
 }
 
 }  // namespace nt

@@ -66,23 +66,25 @@ int main()
         }
         CHECK(tree_row_lo(past, count, count - 1, 1) == past && tree_row_lo(past, count, 0, INT32_MAX) == (past >= INT32_MAX ? 1 : 0));
     }
-    // what a program walks: all that some token may see, each key in one share, shares beginning at multiples of the block; a past beyond the table's reach: its last
-    // position and the new ones
+    // what the programs of a sequence walk: all that some token may see, each key in one program's blocks; a past beyond the table's reach: its last position and the new ones
     for (int i = 0; i < 20000; ++i) {
-        const int32_t count = (int32_t)in(1, 90), length = (int32_t)in(0, 400), window = in(0, 1) ? (int32_t)in(1, 200) : 0, past = length - count;
-        const int32_t capacity = in(0, 2) ? 1000 : (int32_t)in(0, 400);
+        const int32_t count = (int32_t)in(0, 90), length = (int32_t)in(0, 400), window = in(0, 1) ? (int32_t)in(1, 200) : 0, past = length - count;
+        const int32_t capacity = in(0, 2) ? 1000 : (int32_t)in(0, 400), block = in(0, 1) ? 32 : 64;
         const Sequence q{0, count, length};
-        const int32_t block = in(0, 1) ? 32 : 64, splits = (int32_t)in(1, 5), share = block * (int32_t)in(1, 3);
+        const KeyRange k = tree_range(q, window, capacity);
+        const int32_t n = tree_blocks(q, window, block, capacity);
+        CHECK(n == 0 || count > 0);
+        CHECK(n > 0 || count == 0);
         std::vector<int> taken(401, 0);
-        int32_t next = -1;
-        for (int s = 0; s < splits; ++s) {
-            const KeyRange k = tree_range(q, window, s, splits, share, block, capacity);
-            CHECK(0 <= k.lo && k.lo <= k.hi && k.hi <= length);
-            if (s > 0 && k.lo < k.hi) CHECK(k.lo % block == 0 && k.lo == next);
-            if (k.lo < k.hi) next = k.hi;
-            for (int j = k.lo; j < k.hi; ++j) ++taken[j];
+        for (int32_t from = 0; from < n;) {
+            const int32_t to = (int32_t)in(from + 1, n);
+            const KeyRange p = tree_part(k, block, n, from, to);
+            if (from) CHECK(p.lo % block == 0);
+            for (int j = p.lo; j < p.hi; ++j) ++taken[j];
+            CHECK(p.lo >= k.lo && p.hi <= k.hi && (p.hi - 1) / block - p.lo / block < to - from);
+            from = to;
         }
-        for (int32_t j = 0; j < length; ++j) {
+        for (int32_t j = 0; j < length && count; ++j) {
             const bool walked = past > capacity ? j >= past - 1 : j >= past || !window || j > past - window;
             CHECK(taken[j] <= 1 && (!walked || taken[j] == 1));
         }
