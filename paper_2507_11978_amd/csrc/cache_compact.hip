@@ -24,6 +24,14 @@ struct CompactArgs {
     Divider page;
 };
 
+template <typename Piece>
+__device__ __forceinline__ Piece piece_at(const char *p)
+{
+    Piece v;
+    __builtin_memcpy(&v, p, sizeof(Piece));
+    return v;
+}
+
 template <int BYTES, int LANES>
 __global__ __launch_bounds__(256) void cache_compact_kernel(const CompactArgs g)
 {
@@ -41,26 +49,34 @@ __global__ __launch_bounds__(256) void cache_compact_kernel(const CompactArgs g)
         Piece kr[kCompactAhead], vr[kCompactAhead];
         float ks[kCompactAhead], vs[kCompactAhead];
         int32_t to[kCompactAhead], at[kCompactAhead];          // page (-1: nothing to move) and place
+        int32_t from[kCompactAhead], place[kCompactAhead], id[2][kCompactAhead];
+        uint32_t fe[kCompactAhead], te[kCompactAhead];
+        bool moves[kCompactAhead];
+        // (step by step for all of them, so that the loads of a step are on their way together; what is not to be moved is looked up at its own place)
+#pragma unroll
+        for (int i = 0; i < kCompactAhead; ++i) from[i] = path[k0 + i < count ? k0 + i : k0];
 #pragma unroll
         for (int i = 0; i < kCompactAhead; ++i) {
-            const int32_t k = k0 + i;
-            to[i] = -1;
-            if (k >= count) continue;
-            const int64_t f = past + path[k], t = past + k;
-            if (path[k] <= k || t < 0 || f >= kMostKeys) continue;         // (in place already; of no position)
-            const uint32_t fe = divide((uint32_t)f, g.page), te = divide((uint32_t)t, g.page);
-            const int32_t fp = page_at(pages, fe, g.width, g.pages), tp = page_at(pages, te, g.width, g.pages);
-            if (fp < 0 || tp < 0) continue;
-            const int32_t place = (int32_t)((uint32_t)f - fe * g.page.d);
-            __builtin_memcpy(&kr[i], K + (fp * g.ck_sp + place * g.ck_ss) * BYTES, sizeof(Piece));
-            __builtin_memcpy(&vr[i], V + (fp * g.cv_sp + place * g.cv_ss) * BYTES, sizeof(Piece));
-            if constexpr (BYTES == 1)
-                if (d == 0) {
-                    ks[i] = KS[fp * g.ks_sp + place * g.ks_ss];
-                    vs[i] = VS[fp * g.vs_sp + place * g.vs_ss];
-                }
-            to[i] = tp;
-            at[i] = (int32_t)((uint32_t)t - te * g.page.d);
+            const int64_t f = past + from[i], t = past + k0 + i;
+            moves[i] = k0 + i < count && from[i] > k0 + i && t >= 0 && f < kMostKeys;            // (not in place already; of a position)
+            fe[i] = divide(moves[i] ? (uint32_t)f : 0, g.page);
+            te[i] = divide(moves[i] ? (uint32_t)t : 0, g.page);
+            place[i] = (int32_t)((uint32_t)f - fe[i] * g.page.d);
+            at[i] = (int32_t)((uint32_t)t - te[i] * g.page.d);
+            id[0][i] = pages[entry_read(fe[i], g.width)];
+            id[1][i] = pages[entry_read(te[i], g.width)];
+        }
+#pragma unroll
+        for (int i = 0; i < kCompactAhead; ++i) {
+            const bool ok = moves[i] && names_page(fe[i], id[0][i], g.width, g.pages) && names_page(te[i], id[1][i], g.width, g.pages);
+            to[i] = ok ? id[1][i] : -1;
+            const int64_t fp = ok ? id[0][i] : 0, p = ok ? place[i] : 0;   // (nothing to move: the cache's first row, for nothing)
+            kr[i] = piece_at<Piece>(K + (fp * g.ck_sp + p * g.ck_ss) * BYTES);
+            vr[i] = piece_at<Piece>(V + (fp * g.cv_sp + p * g.cv_ss) * BYTES);
+            if constexpr (BYTES == 1) {
+                ks[i] = KS[fp * g.ks_sp + p * g.ks_ss];
+                vs[i] = VS[fp * g.vs_sp + p * g.vs_ss];
+            }
         }
 #pragma unroll
         for (int i = 0; i < kCompactAhead; ++i) {

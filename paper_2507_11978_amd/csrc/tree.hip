@@ -10,11 +10,18 @@
 // Where no child stands the next token is the first t with w(0) + .. + w(t) > r sum w.  Without q the drafts are taken as certain: stands if u m < w(x); if not, m -= w(x),
 // w(x) = 0.  (The next token is then distributed as the target's row would have it, whatever was drafted: a child is tried with the probability that what is left
 // of p gives it over the probability that it was drafted with, and what is left is p less what was tried.)  Sums and comparisons in 64 bits: a token changes where they are off.
+//
+// What has to be read are a few numbers of each draft, and the rows p and q of the node where the walk ends (and of those where more than one child is tried, for m).  One unit reads
+// 128000 words of both in 20 us, the chip 64 of them in 14: the rows are summed in chunks by all of it, then the chunk is searched in which the sum passes its goal.
+// Measured: 64 trees of 24 drafts, 128000 words fp32 64 us (each walk meets two or three such nodes, 21 us of sums, the chain of launches and loads the rest), one chain of 6, 32000
+// words, 11.4 us: walk 3.1, sums 1.9, search 4.8 us, each a chain of loads.
+#include <algorithm>
 #include <type_traits>
 
 #include "gemm_fast.h"
 #include "kernels.h"
 #include "paged_index.h"
+#include "workspace.h"
 
 namespace nt {
 
@@ -83,6 +90,7 @@ nt_status launch_tree_masks(const int32_t *parents, const int32_t *starts, int64
 // ----------------------------------------------------------------------------------------------------- verification
 constexpr int kVerifyThreads = 1024, kVerifyWaves = kVerifyThreads / 64;
 constexpr int kMostTried = 64;                                             // children of a node
+constexpr int kMostChunks = 256;                                           // of a row
 
 struct VerifyArgs {
     const void *target, *draft;
@@ -93,10 +101,29 @@ struct VerifyArgs {
     int64_t *next;
     int64_t t_st, d_st, p_sb;
     int32_t T, V, moves;
+    // in rounds: where each walk is, and sums of its row in chunks
+    struct VerifyState *state;
+    double *sums;
+    int32_t chunk, chunks;
+};
+
+struct Walk {
+    int32_t node, accepted, tried, at;                                     // tokens before `at` have been passed
+};
+
+struct VerifyState {
+    Walk walk;
+    int32_t done, summed;                                                  // the walk has ended; the sums are of where it did
+    double over[kMostTried];
+    int64_t gone[kMostTried];
 };
 
 // What is not a positive finite number has no weight
-__device__ __forceinline__ double weight_of(float v) { return v > 0.f && v < INFINITY ? (double)v : 0.0; }
+__device__ __forceinline__ double weight_of(float v)
+{
+    constexpr int POSITIVE_SUBNORMAL = 1 << 7, POSITIVE_NORMAL = 1 << 8;
+    return (double)(__builtin_amdgcn_classf(v, POSITIVE_SUBNORMAL | POSITIVE_NORMAL) ? v : 0.f);
+}
 
 template <typename T>
 __device__ __forceinline__ float as_float(T v)
@@ -108,52 +135,98 @@ __device__ __forceinline__ float as_float(T v)
 // A node's row as the walk leaves it: what is left of p after `tried` rejections
 template <typename T, bool DRAFT>
 struct Left {
-    static constexpr int N = 16 / sizeof(T);                               // elements of one load
+    static constexpr int N = 16 / sizeof(T), DEEP = 16 / N;                // elements of one load, loads of a row on their way
+    struct Piece {
+        T v[N];
+    };
     const T *p, *q;
-    const double *mass;                                                    // (DRAFT) m before rejection number j
+    const double *over;                                                    // (DRAFT) 1 / m before rejection number j, 0 where m was 0
     const int64_t *gone;                                                   // (not DRAFT) tokens whose weight is 0
     int32_t tried;
 
+    // FEW: of no rejections, or of one (DRAFT; m is 1 at first)
+    static constexpr int ANY = 2;
+    template <int FEW>
     __device__ __forceinline__ double one(float pv, float qv, int32_t t) const
     {
         double w = weight_of(pv);
+        if constexpr (FEW == 0) return w;
         if constexpr (DRAFT) {
             const double q1 = weight_of(qv);
-            for (int j = 0; j < tried; ++j) {
-                const double m = mass[j];
-                w = m > 0.0 ? (j ? w / m : w) - q1 : 0.0;                  // (m is 1 at first)
-                w = w > 0.0 ? w : 0.0;
-            }
-        } else {
+            w = __builtin_fmax(w - q1, 0.0);
+            if constexpr (FEW != 1)
+                for (int j = 1; j < tried; ++j) w = __builtin_fmax(w * over[j] - q1, 0.0);
+        } else if constexpr (FEW == ANY) {
             for (int j = 0; j < tried; ++j) w = gone[j] == t ? 0.0 : w;
         }
         return w;
     }
+    // whether one of N tokens from t on is gone
+    __device__ __forceinline__ bool any_gone(int64_t t) const
+    {
+        bool any = false;
+        if constexpr (!DRAFT)
+            for (int j = 0; j < tried; ++j) any = any | ((uint64_t)(gone[j] - t) < (uint64_t)N);
+        return any;
+    }
+    __device__ __forceinline__ double weight(float pv, float qv, int32_t t) const { return tried ? one<ANY>(pv, qv, t) : one<0>(pv, qv, t); }
+
     // weights of N elements from t on, those from `hi` on are 0
     __device__ __forceinline__ void load(int32_t t, int32_t hi, double (&w)[N]) const
     {
-        T pv[N], qv[N];
+        Piece pv, qv;
         if (t + N <= hi) {
-            __builtin_memcpy(pv, p + t, 16);
-            if (DRAFT && tried) __builtin_memcpy(qv, q + t, 16);
+            __builtin_memcpy(&pv, p + t, 16);
+            if (DRAFT) __builtin_memcpy(&qv, q + t, 16);
 #pragma unroll
-            for (int i = 0; i < N; ++i) w[i] = one(as_float(pv[i]), DRAFT && tried ? as_float(qv[i]) : 0.f, t + i);
+            for (int i = 0; i < N; ++i) w[i] = weight(as_float(pv.v[i]), DRAFT ? as_float(qv.v[i]) : 0.f, t + i);
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) w[i] = t + i < hi ? one(as_float(p[t + i]), DRAFT && tried ? as_float(q[t + i]) : 0.f, t + i) : 0.0;
+            for (int i = 0; i < N; ++i) w[i] = t + i < hi ? weight(as_float(p[t + i]), DRAFT ? as_float(q[t + i]) : 0.f, t + i) : 0.0;
         }
+    }
+    template <int FEW>
+    __device__ __forceinline__ double sum_of(int32_t lo, int32_t hi, int lane, int lanes) const
+    {
+        constexpr bool BOTH = DRAFT && FEW > 0;
+        double s[DEEP] = {};
+        int64_t t = lo + (int64_t)lane * N;
+        const int64_t step = (int64_t)lanes * N;
+        for (; t + (DEEP - 1) * step + N <= hi; t += DEEP * step) {
+            Piece pv[DEEP], qv[BOTH ? DEEP : 1];
+#pragma unroll
+            for (int d = 0; d < DEEP; ++d) __builtin_memcpy(&pv[d], p + t + d * step, 16);
+            if constexpr (BOTH)
+#pragma unroll
+                for (int d = 0; d < DEEP; ++d) __builtin_memcpy(&qv[d], q + t + d * step, 16);
+#pragma unroll
+            for (int d = 0; d < DEEP; ++d) {
+                if (!DRAFT && FEW > 0 && any_gone(t + d * step)) {
+                    double w[N];
+                    load((int32_t)(t + d * step), hi, w);
+#pragma unroll
+                    for (int i = 0; i < N; ++i) s[d] += w[i];
+                    continue;
+                }
+#pragma unroll
+                for (int i = 0; i < N; ++i) s[d] += one<DRAFT ? FEW : 0>(as_float(pv[d].v[i]), BOTH ? as_float(qv[BOTH ? d : 0].v[i]) : 0.f, (int32_t)(t + d * step) + i);
+            }
+        }
+        for (; t < hi; t += step) {
+            double w[N];
+            load((int32_t)t, hi, w);
+#pragma unroll
+            for (int i = 0; i < N; ++i) s[0] += w[i];
+        }
+        double all = s[0];
+#pragma unroll
+        for (int d = 1; d < DEEP; ++d) all += s[d];
+        return all;
     }
     // this lane's part of the sum over [lo, hi), `lanes` lanes side by side
     __device__ __forceinline__ double sum(int32_t lo, int32_t hi, int lane, int lanes) const
     {
-        double s = 0.0;
-        for (int64_t t = lo + (int64_t)lane * N; t < hi; t += (int64_t)lanes * N) {
-            double w[N];
-            load((int32_t)t, hi, w);
-#pragma unroll
-            for (int i = 0; i < N; ++i) s += w[i];
-        }
-        return s;
+        return tried == 0 ? sum_of<0>(lo, hi, lane, lanes) : DRAFT && tried == 1 ? sum_of<1>(lo, hi, lane, lanes) : sum_of<ANY>(lo, hi, lane, lanes);
     }
 };
 
@@ -164,17 +237,20 @@ __device__ __forceinline__ double wave_sum(double v)
     return v;
 }
 
-// Sum over the workgroup, in all threads, added in a fixed order
+// Sum over the workgroup of THREADS, in all threads, added in a fixed order
+template <int THREADS>
 __device__ __forceinline__ double group_sum(double v, double *scratch)
 {
     v = wave_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
-    __syncthreads();
-    double s = 0.0;
+    if constexpr (THREADS > 64) {
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+        __syncthreads();
+        v = 0.0;
 #pragma unroll
-    for (int w = 0; w < kVerifyWaves; ++w) s += scratch[w];
-    return s;
+        for (int w = 0; w < THREADS / 64; ++w) v += scratch[w];
+    }
+    return v;
 }
 
 // The first element of [lo, hi) whose weight brings the sum, `before` ahead of lo, above `goal`; rounding may leave none: then the last with a weight, -1 if there is
@@ -248,105 +324,288 @@ __device__ int32_t find_above(const Left<T, DRAFT> &left, int32_t lo, int32_t hi
             }
         }
     }
-    if (above != 0x7fffffff) atomicMin(&found[0], above);
-    if (last >= 0) atomicMax(&found[1], last);
+    // (one lane of a wavefront: its first, its last; 1024 atomics to one place take 6 us)
+    const uint64_t some = __ballot(above != 0x7fffffff), any = __ballot(last >= 0);
+    if (some && lane == __builtin_ctzll(some)) atomicMin(&found[0], above);
+    if (any && lane == 63 - __builtin_clzll(any)) atomicMax(&found[1], last);
     __syncthreads();
     const int32_t a = found[0], l = found[1];
     __syncthreads();
     return a != 0x7fffffff ? a : l;
 }
 
-// A workgroup to a sequence: the walk, which every wavefront makes for itself (a token to a lane, its numbers loaded ahead of it), and the next token.
-template <typename T, bool DRAFT>
-__global__ __launch_bounds__(kVerifyThreads) void verify_tree_kernel(const VerifyArgs g)
+// The walk, which every wavefront makes for itself (a token to a lane, its numbers loaded ahead of it).  m: after the `tried` rejections, if known.  False: m is needed and not known
+// (SELF: worked out here).
+template <typename T, bool DRAFT, bool SELF, int THREADS>
+__device__ __forceinline__ bool walk_tree(const VerifyArgs &g, const int32_t first, const int32_t count, int32_t *path, Walk &s, double m, bool known, double *over, int64_t *gone,
+                                          double *scratch)
 {
-    __shared__ double scratch[kVerifyWaves], mass[kMostTried];
-    __shared__ int64_t gone[kMostTried];
-    __shared__ int32_t found[2];
-    const int tid = threadIdx.x, lane = tid & 63, b = blockIdx.x;
-    const int32_t first = clamp_i32(g.starts[b], 0, g.T), count = clamp_i32(g.starts[b + 1], first, g.T) - first;
-    int32_t *path = g.path + b * g.p_sb;
+    const int tid = threadIdx.x, lane = tid & 63;
     auto target_row = [&](int32_t node) { return (const T *)g.target + (int64_t)(first + node) * g.t_st; };
     auto draft_row = [&](int32_t node) { return DRAFT ? (const T *)g.draft + (int64_t)(first + node) * g.d_st : nullptr; };
-
-    int32_t node = 0, accepted = count && g.moves ? 1 : 0, tried = 0, known = 0;        // known: rejections that m is of
-    double m = 1.0;
-    if (tid == 0 && accepted) path[0] = 0;
-    for (int32_t c = 0; c < count && accepted && accepted < g.moves; c += 64) {
-        const int32_t i = c + lane, t = first + (i < count ? i : 0);
+    while (s.at < count && s.accepted < g.moves) {
+        const int32_t c = s.at & ~63, i = c + lane, t = first + (i < count ? i : 0);
         const int32_t parent = i < count && i > 0 ? g.parents[t] : -1;
         const int64_t x = g.ids[t];
         const float u = g.uniform[t];
         const bool real = parent >= 0 && parent < i && x >= 0 && x < g.V;  // (a token of no vocabulary is passed over)
-        const double p = real ? weight_of(as_float(target_row(parent)[x])) : 0.0, q = DRAFT ? (real ? weight_of(as_float(draft_row(parent)[x])) : 0.0) : 1.0;
-        uint64_t behind = ~0ull;                                           // those behind the last one that was tried
-        while (accepted < g.moves) {
-            const uint64_t children = __ballot(real && parent == node) & behind;
-            if (!children || tried == kMostTried) break;
+        const float p = real ? as_float(target_row(parent)[x]) : 0.f, q = DRAFT && real ? as_float(draft_row(parent)[x]) : 0.f;
+        while (s.accepted < g.moves) {
+            const uint64_t children = __ballot(real && parent == s.node && i >= s.at);
+            if (!children || s.tried == kMostTried) break;
             const int l = __builtin_ctzll(children);
-            behind = l == 63 ? 0 : ~0ull << (l + 1);
-            const double pl = __shfl(p, l, 64), ql = __shfl(q, l, 64);
-            const float ul = __shfl(u, l, 64);
+            const float pl = __shfl(p, l, 64), ql = __shfl(q, l, 64), ul = __shfl(u, l, 64);
             const int64_t xl = __shfl(x, l, 64);
-            const Left<T, DRAFT> left{target_row(node), draft_row(node), mass, gone, tried};
-            if (DRAFT && known < tried) {
-                m = group_sum(left.sum(0, g.V, tid, kVerifyThreads), scratch);
-                known = tried;
+            const Left<T, DRAFT> left{target_row(s.node), draft_row(s.node), over, gone, s.tried};
+            if (DRAFT && !known) {
+                if constexpr (!SELF) return false;
+                m = group_sum<THREADS>(left.sum(0, g.V, tid, THREADS), scratch);
+                known = true;
             }
-            // (p and q have been through weight_of: once more changes nothing)
-            double w = pl;
-            if constexpr (DRAFT) {
-                for (int j = 0; j < tried; ++j) {
-                    const double d = mass[j];
-                    w = d > 0.0 ? (j ? w / d : w) - ql : 0.0;
-                    w = w > 0.0 ? w : 0.0;
-                }
-            } else {
-                for (int j = 0; j < tried; ++j) w = gone[j] == xl ? 0.0 : w;
-            }
-            if ((double)ul * ql * m < w) {
-                node = c + l;
-                if (tid == 0) path[accepted] = node;
-                ++accepted;
-                tried = known = 0;
+            const double w = left.weight(pl, ql, (int32_t)xl);
+            s.at = c + l + 1;
+            if ((double)ul * (DRAFT ? weight_of(ql) : 1.0) * m < w) {
+                s.node = c + l;
+                if (tid == 0) path[s.accepted] = s.node;
+                ++s.accepted;
+                s.tried = 0;
                 m = 1.0;
             } else {
                 __syncthreads();                                           // (all wavefronts are here: they walk alike; what is written below may still be read)
                 if (tid == 0) {
-                    if (DRAFT) mass[tried] = m;
-                    else gone[tried] = xl;
+                    if (DRAFT) over[s.tried] = m > 0.0 ? 1.0 / m : 0.0;
+                    else gone[s.tried] = xl;
                 }
                 __syncthreads();
-                if (!DRAFT) m = m - w > 0.0 ? m - w : 0.0;
-                ++tried;
+                if (DRAFT) known = false;
+                else m = m - w > 0.0 ? m - w : 0.0;
+                ++s.tried;
             }
         }
+        s.at = s.at > c + 64 ? s.at : c + 64;
     }
+    return true;
+}
 
-    int64_t next = -1;
-    if (count > 0) {
-        Left<T, DRAFT> left{target_row(node), draft_row(node), mass, gone, tried};
-        double total = group_sum(left.sum(0, g.V, tid, kVerifyThreads), scratch);
-        if (!(total > 0.0) && tried) {                                     // (nothing is left: the target's row as it is)
-            left.tried = 0;
-            total = group_sum(left.sum(0, g.V, tid, kVerifyThreads), scratch);
-        }
-        const float r = g.last_uniform[b];
-        if (total > 0.0) next = find_above(left, 0, g.V, 0.0, r > 0.f ? (double)r * total : 0.0, scratch, found);
-    }
-    for (int32_t k = accepted + tid; k < g.moves; k += kVerifyThreads) path[k] = -1;
-    if (tid == 0) {
-        g.accepted[b] = accepted;
-        g.next[b] = next;
-        if (g.new_lengths) g.new_lengths[b] = g.lengths[b] - count + accepted;
+// What is told of a sequence where its walk ends
+__device__ __forceinline__ void tell(const VerifyArgs &g, int b, int32_t count, const Walk &s, int threads)
+{
+    for (int64_t k = s.accepted + (int64_t)threadIdx.x; k < g.moves; k += threads) g.path[b * g.p_sb + k] = -1;
+    if (threadIdx.x == 0) {
+        g.accepted[b] = s.accepted;
+        if (g.new_lengths) g.new_lengths[b] = g.lengths[b] - count + s.accepted;
     }
 }
 
-template <typename T>
-static void launch_verify_type(const VerifyArgs &a, int64_t sequences, hipStream_t s)
+// The next token, from the node's row as it is left, `total` its sum and `before` that ahead of lo; where nothing is left the target's row as it is
+template <typename T, bool DRAFT>
+__device__ __forceinline__ int64_t next_token(const VerifyArgs &g, int b, Left<T, DRAFT> left, int32_t lo, int32_t hi, double before, double total, double *scratch, int32_t *found)
 {
-    if (a.draft) hipLaunchKernelGGL((verify_tree_kernel<T, true>), dim3((unsigned)sequences), dim3(kVerifyThreads), 0, s, a);
-    else hipLaunchKernelGGL((verify_tree_kernel<T, false>), dim3((unsigned)sequences), dim3(kVerifyThreads), 0, s, a);
+    if (!(total > 0.0) && left.tried) {
+        left.tried = 0;
+        lo = 0;
+        hi = g.V;
+        before = 0.0;
+        total = group_sum<kVerifyThreads>(left.sum(0, g.V, threadIdx.x, kVerifyThreads), scratch);
+    }
+    const float r = g.last_uniform[b];
+    return total > 0.0 ? find_above(left, lo, hi, before, r > 0.f ? (double)r * total : 0.0, scratch, found) : -1;
+}
+
+__device__ __forceinline__ int32_t first_of(const VerifyArgs &g, int b) { return clamp_i32(g.starts[b], 0, g.T); }
+__device__ __forceinline__ int32_t count_of(const VerifyArgs &g, int b) { return clamp_i32(g.starts[b + 1], first_of(g, b), g.T) - first_of(g, b); }
+
+// A workgroup to a sequence: short rows
+template <typename T, bool DRAFT>
+__global__ __launch_bounds__(kVerifyThreads) void verify_tree_kernel(const VerifyArgs g)
+{
+    __shared__ double scratch[kVerifyWaves], over[kMostTried];
+    __shared__ int64_t gone[kMostTried];
+    __shared__ int32_t found[2];
+    const int b = blockIdx.x;
+    const int32_t first = first_of(g, b), count = count_of(g, b);
+    int32_t *path = g.path + b * g.p_sb;
+    Walk s{0, count ? 1 : 0, 0, 1};
+    if (threadIdx.x == 0 && count) path[0] = 0;
+    if (count) walk_tree<T, DRAFT, true, kVerifyThreads>(g, first, count, path, s, 1.0, true, over, gone, scratch);
+    int64_t next = -1;
+    if (count) {
+        const int64_t row = first + s.node;
+        const Left<T, DRAFT> left{(const T *)g.target + row * g.t_st, DRAFT ? (const T *)g.draft + row * g.d_st : nullptr, over, gone, s.tried};
+        const double total = group_sum<kVerifyThreads>(left.sum(0, g.V, threadIdx.x, kVerifyThreads), scratch);
+        next = next_token(g, b, left, 0, g.V, 0.0, total, scratch, found);
+    }
+    tell(g, b, count, s, kVerifyThreads);
+    if (threadIdx.x == 0) g.next[b] = next;
+}
+
+// ---- the same in rounds: a walk goes as far as it knows m, and the sums of the rows that it needs are dealt out over the chip
+// A sequence's sums of chunks: PER side by side to a lane, in every wavefront alike
+struct Chunks {
+    static constexpr int PER = kMostChunks / 64;
+    double v[PER], before = 0.0;
+
+    __device__ __forceinline__ Chunks(const VerifyArgs &g, int b)
+    {
+        const int c = PER * (threadIdx.x & 63);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[i] = c + i < g.chunks ? g.sums[(int64_t)b * g.chunks + c + i] : 0.0;
+    }
+    // their sum; and the first chunk that brings it above share * sum (the last that has anything, if rounding leaves none; -1: none has), `before` what is ahead of it
+    __device__ __forceinline__ int find(double share, double *total)
+    {
+        const int lane = threadIdx.x & 63;
+        double mine = 0.0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) mine += v[i];
+        double upto = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const double other = __shfl_up(upto, d, 64);
+            if (lane >= d) upto += other;
+        }
+        *total = __shfl(upto, 63, 64);
+        const double goal = share * *total;
+        int above = -1, last = -1;
+        double run = upto - mine, at_above = 0.0, at_last = 0.0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (above < 0 && run + v[i] > goal) {
+                above = i;
+                at_above = run;
+            }
+            if (v[i] > 0.0) {
+                last = i;
+                at_last = run;
+            }
+            run += v[i];
+        }
+        const uint64_t some = __ballot(above >= 0), any = __ballot(last >= 0);
+        if (!any) return -1;
+        const int l = some ? __builtin_ctzll(some) : 63 - __builtin_clzll(any);
+        before = __shfl(some ? at_above : at_last, l, 64);
+        return PER * l + __shfl(some ? above : last, l, 64);
+    }
+};
+
+template <typename T, bool DRAFT, bool FIRST, bool LAST>
+__global__ __launch_bounds__(LAST ? kVerifyThreads : 64) void verify_walk_kernel(const VerifyArgs g)
+{
+    constexpr int THREADS = LAST ? kVerifyThreads : 64;
+    __shared__ double scratch[kVerifyWaves], over[kMostTried];
+    __shared__ int64_t gone[kMostTried];
+    const int b = blockIdx.x, tid = threadIdx.x;
+    const int32_t first = first_of(g, b), count = count_of(g, b);
+    VerifyState *state = g.state + b;
+    int32_t *path = g.path + b * g.p_sb;
+    Walk s{0, count ? 1 : 0, 0, 1};
+    double m = 1.0;
+    if constexpr (FIRST) {
+        if (tid == 0 && count) path[0] = 0;
+    } else {
+        if (state->done) {
+            if (tid == 0) state->summed = 1;
+            return;
+        }
+        s = state->walk;
+        if (DRAFT && tid < s.tried) over[tid] = state->over[tid];
+        Chunks(g, b).find(0.0, &m);
+        __syncthreads();
+    }
+    const bool done = !count || walk_tree<T, DRAFT, LAST, THREADS>(g, first, count, path, s, m, true, over, gone, scratch);
+    __syncthreads();
+    if (tid < s.tried) {
+        if constexpr (DRAFT) state->over[tid] = over[tid];
+        else state->gone[tid] = gone[tid];
+    }
+    if (tid == 0) {
+        state->walk = s;
+        state->done = done;
+        state->summed = 0;
+    }
+    if (done) tell(g, b, count, s, THREADS);
+}
+
+template <typename T, bool DRAFT>
+__global__ __launch_bounds__(256) void verify_sums_kernel(const VerifyArgs g)
+{
+    __shared__ double scratch[4];
+    const int b = blockIdx.x / g.chunks, c = blockIdx.x - b * g.chunks;
+    const VerifyState *state = g.state + b;
+    const int32_t count = count_of(g, b);
+    if (state->summed || !count) return;
+    const int64_t row = first_of(g, b) + state->walk.node;
+    const Left<T, DRAFT> left{(const T *)g.target + row * g.t_st, DRAFT ? (const T *)g.draft + row * g.d_st : nullptr, state->over, state->gone, state->walk.tried};
+    const int32_t lo = c * g.chunk, hi = g.V - lo < g.chunk ? g.V : lo + g.chunk;
+    const double sum = group_sum<256>(left.sum(lo, hi, threadIdx.x, 256), scratch);
+    if (threadIdx.x == 0) g.sums[(int64_t)b * g.chunks + c] = sum;
+}
+
+template <typename T, bool DRAFT>
+__global__ __launch_bounds__(kVerifyThreads) void verify_pick_kernel(const VerifyArgs g)
+{
+    __shared__ double scratch[kVerifyWaves];
+    __shared__ int32_t found[2];
+    const int b = blockIdx.x, tid = threadIdx.x;
+    const VerifyState *state = g.state + b;
+    int64_t next = -1;
+    if (count_of(g, b)) {
+        Chunks sums(g, b);
+        const float r = g.last_uniform[b];
+        double total;
+        const int found_at = sums.find(r > 0.f ? (double)r : 0.0, &total), chosen = found_at < 0 ? 0 : found_at;
+        const int64_t row = first_of(g, b) + state->walk.node;
+        const Left<T, DRAFT> left{(const T *)g.target + row * g.t_st, DRAFT ? (const T *)g.draft + row * g.d_st : nullptr, state->over, state->gone, state->walk.tried};
+        const int32_t lo = chosen * g.chunk, hi = g.V - lo < g.chunk ? g.V : lo + g.chunk;
+        next = next_token(g, b, left, lo, hi, sums.before, total, scratch, found);
+    }
+    if (tid == 0) g.next[b] = next;
+}
+
+template <typename T, bool DRAFT>
+static nt_status launch_verify_kind(VerifyArgs &a, int64_t sequences, hipStream_t s)
+{
+    const dim3 each((unsigned)sequences);
+    constexpr int N = 16 / sizeof(T);
+    // Chunks for some 2048 workgroups in all, of whole rounds of loads
+    const int64_t least = 256 * N, wanted = std::max<int64_t>(1, std::min<int64_t>(kMostChunks, 2048 / sequences));
+    const int64_t chunk = std::max(least, ((a.V + wanted - 1) / wanted + least - 1) / least * least), chunks = (a.V + chunk - 1) / chunk;
+    // A unit reads some 40 GB/s: of rows of 64 KB (both) and less one has enough (1 sequence, 8000 words 10.3 us, 10.8 in three launches; 32000 15.1, 11.4; 128000 30.9, 11.3).  Rounds
+    // before the last, whose sums are a unit's own work, are 3 us each where no walk needs one: only for long rows of trees that are likely to (us, 64 trees of 24, 128000 words: no round 98,
+    // four 64, six 77; 64000 71, 58; 32000 47, 53; chains of 6, 128000: 11.3, 13.7 with one).
+    const int64_t row_bytes = (int64_t)a.V * (int64_t)sizeof(T) * (DRAFT ? 2 : 1);
+    const int rounds = DRAFT && row_bytes > (256 << 10) ? (int)std::min<int64_t>(4, std::max<int64_t>(0, (a.T / sequences - 3) / 5)) : 0;
+    WorkspaceLease lease;
+    char *ws = nullptr;
+    if (row_bytes > (64 << 10) && sequences * chunks <= kMaxWorkgroups) ws = (char *)lease.acquire((size_t)sequences * (sizeof(VerifyState) + (size_t)chunks * 8), s);
+    if (!ws) {
+        hipLaunchKernelGGL((verify_tree_kernel<T, DRAFT>), each, dim3(kVerifyThreads), 0, s, a);
+        return check_launch("verify_tree_kernel");
+    }
+    a.state = (VerifyState *)ws;
+    a.sums = (double *)(ws + (size_t)sequences * sizeof(VerifyState));
+    a.chunk = (int32_t)chunk;
+    a.chunks = (int32_t)chunks;
+    const dim3 all((unsigned)(sequences * chunks));
+    if (rounds) {
+        hipLaunchKernelGGL((verify_walk_kernel<T, DRAFT, true, false>), each, dim3(64), 0, s, a);
+        for (int i = 1; i <= rounds; ++i) {
+            hipLaunchKernelGGL((verify_sums_kernel<T, DRAFT>), all, dim3(256), 0, s, a);
+            if (i < rounds) hipLaunchKernelGGL((verify_walk_kernel<T, DRAFT, false, false>), each, dim3(64), 0, s, a);
+            else hipLaunchKernelGGL((verify_walk_kernel<T, DRAFT, false, true>), each, dim3(kVerifyThreads), 0, s, a);
+        }
+    } else {
+        hipLaunchKernelGGL((verify_walk_kernel<T, DRAFT, true, true>), each, dim3(kVerifyThreads), 0, s, a);
+    }
+    hipLaunchKernelGGL((verify_sums_kernel<T, DRAFT>), all, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((verify_pick_kernel<T, DRAFT>), each, dim3(kVerifyThreads), 0, s, a);
+    return check_launch("verify_walk_kernel");
+}
+
+template <typename T>
+static nt_status launch_verify_type(VerifyArgs &a, int64_t sequences, hipStream_t s)
+{
+    return a.draft ? launch_verify_kind<T, true>(a, sequences, s) : launch_verify_kind<T, false>(a, sequences, s);
 }
 
 nt_status launch_verify_tree(const void *target, const nt_tensor_desc *dt, const void *draft, const nt_tensor_desc *dd, const int64_t *ids, const int32_t *parents,
@@ -372,13 +631,12 @@ nt_status launch_verify_tree(const void *target, const nt_tensor_desc *dt, const
     if (sequences == 0) return NT_OK;
     if (!starts || !last_uniform || !path || !accepted || !next || (dt->size[0] && (!ids || !parents || !uniform)) || (dt->size[0] && dt->size[1] && !target))
         return fail(NT_ERR_INVALID_ARG, "null device pointer");
-    const VerifyArgs a{target, draft, ids, parents, starts, lengths, uniform, last_uniform, path, accepted, new_lengths, next,
-                       dt->stride[0], dd ? dd->stride[0] : 0, dp->stride[0], (int32_t)dt->size[0], (int32_t)dt->size[1], (int32_t)dp->size[1]};
+    VerifyArgs a{target, draft, ids, parents, starts, lengths, uniform, last_uniform, path, accepted, new_lengths, next,
+                 dt->stride[0], dd ? dd->stride[0] : 0, dp->stride[0], (int32_t)dt->size[0], (int32_t)dt->size[1], (int32_t)dp->size[1], nullptr, nullptr, 0, 0};
     hipStream_t s = (hipStream_t)stream;
-    if (dtype == NT_F32) launch_verify_type<float>(a, sequences, s);
-    else if (dtype == NT_F16) launch_verify_type<_Float16>(a, sequences, s);
-    else launch_verify_type<__bf16>(a, sequences, s);
-    return check_launch("verify_tree_kernel");
+    if (dtype == NT_F32) return launch_verify_type<float>(a, sequences, s);
+    if (dtype == NT_F16) return launch_verify_type<_Float16>(a, sequences, s);
+    return launch_verify_type<__bf16>(a, sequences, s);
 }
 
 }  // namespace nt
