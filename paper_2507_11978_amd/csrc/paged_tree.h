@@ -16,12 +16,12 @@ namespace nt {
 // us, graph replays, 32 x 17 to 4096 keys x 32/8 heads x 128 bf16, 16 tokens each: 99.5 with 0, 94.3 with 2, 90.5 with 4, 91 with 6 and 8; 128 x 500 to 1000 97.6 / 88.5 / 89 / 88.
 constexpr int kTreeBegin = 4;
 
-// Blocks to a program, beginnings among them.  Short runs go to half of the programs, one to a unit: fewer shares to join (4 x 2048 to 4096 keys 34.4 us with all, 28.8;
-// 1 x 4096 50.9, 33.1; but the 32 sequences above 90.5, 98, with runs of 22 blocks).
+// Blocks to a program, beginnings among them but for the first sequence's (every program has one at its own start).  Short runs go to half of the programs, one to a unit, where
+// the sequences are few: less shares to join (4 x 2048 to 4096 keys 34.4 us with all, 28.8; 1 x 4096 50.9, 33.1; but 16 x 1 to 3000 keys 37.0, 40.3).
 __device__ __forceinline__ int64_t tree_run(const PagedArgs &g, int64_t all)
 {
-    const int64_t run = (all + g.groups - 1) / g.groups, half = g.groups / 2;
-    return run < 12 && half ? (all + half - 1) / half : run;
+    const int64_t shared = all - kTreeBegin, run = (shared + g.groups - 1) / g.groups, half = g.groups / 2;
+    return run < 12 && half > 4 * g.B ? (shared + half - 1) / half : run;
 }
 
 // The same in all lanes: in scalar registers
@@ -31,9 +31,8 @@ __device__ __forceinline__ int64_t uniform(int64_t v) { return (int64_t)((uint64
 template <bool BF16, int KIND, int SIZE, bool FAST, bool FULL, int GROUPS>
 __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void paged_tree_kernel(const PagedArgs g)
 {
-    constexpr int ROWS = kManyRows / GROUPS, KB = many_keys(SIZE), PER = kTreeSequences / 256;
+    constexpr int ROWS = kManyRows / GROUPS, KB = many_keys(SIZE), PER = kTreeSequences / 64;
     extern __shared__ __attribute__((aligned(1024))) char smem[];
-    __shared__ int64_t before[kTreeSequences + 1], sums[kManyWaves];
     const int32_t capacity = g.width * (int32_t)g.page.d;
 
     // A sequence's heads and row parts on one XCD (workgroups go to the XCDs in turn), near each other in time: what they read lies side by side, or is the same
@@ -42,68 +41,75 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
     const uint32_t inner = (uint32_t)g.Hkv * g.parts, which = program % inner, part = which % g.parts, group = program / inner;
     const int32_t h = which / g.parts;
 
+    // ---- the blocks of each sequence, and before a lane's first: up to PER of them side by side to a lane.  Every wavefront finds and writes the same, and reads what it wrote
+    __shared__ int32_t blocks[PER][64];
+    __shared__ int64_t before[64];
+    const int lane = threadIdx.x & 63, per = (g.B + 63) / 64;
     int64_t start = 0, end = 1;
     if (g.groups) {
-        // ---- the blocks before each sequence: up to PER sequences to a thread
-        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, first = tid * PER;
-        int32_t blocks[PER];
-        int64_t upto = 0;
+        Sequence seq[PER];
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            blocks[i] = first + i < g.B ? tree_blocks(sequence_of(g, first + i), g.window, KB, capacity) : 0;
-            blocks[i] += blocks[i] ? kTreeBegin : 0;
-            upto += blocks[i];
+            if (i < per) seq[i] = sequence_of(g, per * lane + i < g.B ? per * lane + i : g.B - 1);
         }
+        int64_t upto = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (i < per) {
+                const int32_t n = per * lane + i < g.B ? tree_blocks(seq[i], g.window, KB, capacity) : 0;
+                blocks[i][lane] = n ? n + kTreeBegin : 0;
+                upto += n ? n + kTreeBegin : 0;
+            }
         int64_t sum = -upto;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const int64_t other = __shfl_up(upto, d, 64);
             if (lane >= d) upto += other;
         }
-        if (lane == 63) sums[wave] = upto;
-        __syncthreads();
         sum += upto;
-        for (int w = 0; w < wave; ++w) sum += sums[w];
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            if (first + i <= g.B) {
-                before[first + i] = sum;
-                if (blockIdx.x == 0) g.before[first + i] = sum;            // (for the join)
-            }
-            sum += blocks[i];
-        }
-        if (tid == 255 && g.B == kTreeSequences) {
-            before[g.B] = sum;
-            if (blockIdx.x == 0) g.before[g.B] = sum;
-        }
-        __syncthreads();
-        const int64_t all = uniform(before[g.B]), run = tree_run(g, all);
-        start = group * run;
+        before[lane] = sum;
+        const int64_t all = uniform(__shfl(upto, 63, 64)), run = tree_run(g, all);
+        start = kTreeBegin + group * run;
         end = start + run < all ? start + run : all;
+        if (blockIdx.x == 0 && threadIdx.x < 64) {                         // (for the join)
+            for (int i = 0; i < per; ++i) {
+                if (per * lane + i < g.B) g.before[per * lane + i] = sum;
+                sum += blocks[i][lane];
+            }
+            if (lane == 0) g.before[g.B] = all;
+        }
     }
 
     for (int64_t at = start; at < end;) {
         int32_t b = group;
-        if (g.groups) {                                                    // the last sequence that begins at or before the block (one that has any)
-            b = 0;
-            for (int up = g.B; up - b > 1;) {
-                const int step = (up - b + 63) / 64, i = b + (threadIdx.x & 63) * step;
-                const uint64_t below = __ballot(i < up && before[i < up ? i : b] <= at);
-                b += (63 - __builtin_clzll(below)) * step;
-                up = b + step < up ? b + step : up;
+        int64_t ahead = 0;                                                 // blocks before sequence b
+        if (g.groups) {
+            // the last sequence that begins at or before the block, of those that have any: in the last lane that begins there with any
+            int64_t sum = before[lane], mine = 0;
+            int32_t which = -1;
+            for (int i = 0; i < per; ++i) {
+                const int32_t n = blocks[i][lane];
+                if (n && sum <= at) {
+                    which = per * lane + i;
+                    mine = sum;
+                }
+                sum += n;
             }
+            const int l = 63 - __builtin_clzll(__ballot(which >= 0));
+            b = uniform(__shfl(which, l, 64));
+            ahead = uniform(__shfl(mine, l, 64));
         }
         const Sequence in_memory = sequence_of(g, b), seq{uniform(in_memory.first), uniform(in_memory.count), uniform(in_memory.length)};
         const KeyRange keys = tree_range(seq, g.window, capacity);
         const int32_t n = tree_blocks(seq, g.window, KB, capacity);
-        const int64_t inside = g.groups ? at - uniform(before[b]) : kTreeBegin;
+        const int64_t inside = g.groups ? at - ahead : kTreeBegin;
         if (!g.groups) end = n;
         const int32_t from = inside > kTreeBegin ? (int32_t)(inside - kTreeBegin) : 0;
         const int64_t until = end - at + inside - kTreeBegin;
         const int32_t to = until < n ? (int32_t)until : n;
         at += n + kTreeBegin - inside;
         if (to <= from) continue;
-        const int64_t slot = (2 * (int64_t)program + (inside <= kTreeBegin && before[b] + kTreeBegin != start)) * ROWS, rows = (int64_t)seq.count * g.G;
+        const int64_t slot = (2 * (int64_t)program + (inside <= kTreeBegin && ahead + kTreeBegin != start)) * ROWS, rows = (int64_t)seq.count * g.G;
         // (rows beyond the caller's bound on new tokens follow, not shared)
         bool due = true;
         for (int64_t r0 = (int64_t)part * ROWS; r0 < rows && (due || from == 0); r0 += (int64_t)g.parts * ROWS) {
@@ -125,7 +131,7 @@ __global__ __launch_bounds__(256) void paged_tree_join_kernel(const PagedArgs g)
     const Sequence seq = sequence_of(g, b);
     const int64_t rows = (int64_t)seq.count * g.G, r0 = (int64_t)part * ROWS;
     if (r0 + 16 * blockIdx.y >= rows) return;
-    const int64_t first = g.before[b] + kTreeBegin, run = tree_run(g, g.before[g.B]), g0 = first / run, g1 = (g.before[b + 1] - 1) / run;
+    const int64_t first = g.before[b], run = tree_run(g, g.before[g.B]), g0 = first / run, g1 = (g.before[b + 1] - 1 - kTreeBegin) / run;
     if (g0 == g1) return;                                                  // (one program has had it all)
     const int d = 4 * (threadIdx.x % LANES);
     if (d >= g.D) return;
