@@ -448,7 +448,7 @@ nt_status nt_verify_tree(const void *target, const nt_tensor_desc *d_target, con
  * p = lengths[b] - accepted[b] the token at position p + path[b][k] goes to position p + k, for all k < accepted[b], as if all were read before any is written.
  * lengths, path, accepted as nt_verify_tree leaves them (a row of path ascends; an entry that is not above its own place is not moved, nor is one whose
  * positions have no page).  caches: a HOST array of n_caches caches (a program's layers) that share the page table, one type and one layout (else
- * NT_ERR_SHAPE_MISMATCH).  Codes and scales are moved as they are. */
+ * NT_ERR_SHAPE_MISMATCH), each once (else NT_ERR_INVALID_ARG).  Codes and scales are moved as they are. */
 nt_status nt_cache_compact(const nt_paged_cache *caches, int64_t n_caches, const int32_t *table, const nt_tensor_desc *d_table, const int32_t *lengths,
                            const int32_t *path, const nt_tensor_desc *d_path, const int32_t *accepted, void *hip_stream);
 

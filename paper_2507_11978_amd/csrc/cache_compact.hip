@@ -148,7 +148,12 @@ nt_status launch_cache_compact(const nt_paged_cache *caches, int64_t n, const in
     a.heads = (int32_t)c.dk->size[2]; a.size = (int32_t)c.dk->size[3]; a.pages = (int32_t)c.dk->size[0];
     a.page = divider_of((uint32_t)c.dk->size[1]);
     a.width = entries_in_reach(dt->size[1], a.page.d); a.moves = (int32_t)dp->size[1];
-    if (a.rows > 0x7fffffffLL) return fail(NT_ERR_UNSUPPORTED, "sequences * heads must be below 2^31");
+    if (a.rows > kMaxWorkgroups) return fail(NT_ERR_UNSUPPORTED, "too many sequences and heads for one launch");
+    // (moved twice at a time, a cache's rows could be read after they were written)
+    for (int64_t i = 0; i < n; ++i)
+        for (int64_t j = 0; j < i; ++j)
+            if (caches[i].k == caches[j].k || caches[i].k == caches[j].v || caches[i].v == caches[j].k || caches[i].v == caches[j].v)
+                return fail(NT_ERR_INVALID_ARG, "a cache is listed twice");
     for (int64_t i = 0; i < n; i += kCompactCaches) {
         const int m = (int)(n - i < kCompactCaches ? n - i : kCompactCaches);
         for (int j = 0; j < m; ++j) {

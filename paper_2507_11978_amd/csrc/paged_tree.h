@@ -1,7 +1,8 @@
 // Attention for trees of drafted tokens over a paged cache: who walks which keys, and the launches for one built head size.
 //
 // Tiles of 128 or 64 rows (token, query head of the group) of one sequence and key head, walked as in paged_many.h; with 64 rows two wavefronts share them and two groups of
-// wavefronts the keys of a block, so that all four SIMDs multiply.
+// wavefronts the keys of a block, so that all four SIMDs multiply.  Fewer rows go the same way: paged_few.h with masks took 76 us, 67 so, for 32 sequences of 17 to 4096 keys, 16 rows
+// of 128 bf16 a key head, 118 and 72 with 32 rows (its shares are of one length, and write and join more); 15.3 against 17.4 for one sequence of 900, 48 heads x 64.
 //
 // Sequences of a serving batch are of every age, and a program to each is done when the oldest is.  So the blocks of keys of all sequences and heads, one behind the other, are
 // dealt out to as many programs as the units hold, each the same number.  Where a program's run ends inside a sequence's head it leaves its share (reference m, sum l and
@@ -45,7 +46,7 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
     __shared__ int32_t blocks[PER][64];
     __shared__ int64_t before[64];
     const int lane = threadIdx.x & 63, per = (g.B + 63) / 64;
-    int64_t start = 0, end = 1;
+    int64_t start = 0, end = 1, run = 1;
     if (g.groups) {
         Sequence seq[PER];
 #pragma unroll
@@ -68,7 +69,8 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
         }
         sum += upto;
         before[lane] = sum;
-        const int64_t all = uniform(__shfl(upto, 63, 64)), run = tree_run(g, all);
+        const int64_t all = uniform(__shfl(upto, 63, 64));
+        run = tree_run(g, all);
         start = kTreeBegin + group * run;
         end = start + run < all ? start + run : all;
         if (blockIdx.x == 0 && threadIdx.x < 64) {                         // (for the join)
@@ -108,16 +110,20 @@ __global__ __launch_bounds__(64 * kManyWaves, many_resident(KIND, SIZE)) void pa
         const int64_t until = end - at + inside - kTreeBegin;
         const int32_t to = until < n ? (int32_t)until : n;
         at += n + kTreeBegin - inside;
-        if (to <= from) continue;
         const int64_t slot = (2 * (int64_t)program + (inside <= kTreeBegin && ahead + kTreeBegin != start)) * ROWS, rows = (int64_t)seq.count * g.G;
-        // (rows beyond the caller's bound on new tokens follow, not shared)
-        bool due = true;
-        for (int64_t r0 = (int64_t)part * ROWS; r0 < rows && (due || from == 0); r0 += (int64_t)g.parts * ROWS) {
-            const bool share = due && (from > 0 || to < n);
-            paged_many_tile<BF16, KIND, SIZE, FAST, FULL, true, GROUPS>(g, smem, b, h, seq, (int)r0, 0, due ? tree_part(keys, KB, n, from, to) : keys,
+        // Rows beyond the caller's bound on new tokens: not shared, tiles of all keys, dealt out to the programs that have blocks of this sequence
+        int64_t sharers = 1, mine = 0;
+        if (g.groups && rows > (int64_t)g.parts * ROWS) {
+            sharers = (ahead + n - 1) / run - ahead / run + 1;
+            mine = (int64_t)group - ahead / run;
+        }
+        int64_t tile = 0;
+        for (int64_t r0 = (int64_t)part * ROWS; r0 < rows; r0 += (int64_t)g.parts * ROWS, ++tile) {
+            if (tile ? tile % sharers != mine : to <= from) continue;      // (workgroup-uniform)
+            const bool share = tile == 0 && (from > 0 || to < n);
+            paged_many_tile<BF16, KIND, SIZE, FAST, FULL, true, GROUPS>(g, smem, b, h, seq, (int)r0, 0, tile ? keys : tree_part(keys, KB, n, from, to),
                                                                         share ? g.part_ml + slot * 2 : nullptr, share ? g.part_o + slot * g.D : nullptr);
             __syncthreads();
-            due = false;
         }
     }
 }

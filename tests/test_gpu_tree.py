@@ -329,6 +329,24 @@ def test_bounds_that_are_too_low_cost_time_only():
     b.check(b.run(max_queries=1))
 
 
+def test_a_table_without_entries():
+    b = Trees([(1, 0), (3, 0)], 4, 2, 64, 16, "f16")
+    b.table = np.zeros((2, 0), np.int64)
+    assert (b.run() == 0).all()
+    b.lengths = [1, 0]
+    got = b.run()
+    assert torch.isnan(got[0]).all() and (got[1:] == 0).all()
+
+
+def test_rows_beyond_the_bound_among_sequences():
+    """A tree far larger than the others', and than the bound: its rows are dealt out among the programs that share its keys."""
+    b = Trees([(1, 100), (300, 900), (2, 500), (1, 3), (150, 150), (1, 700)], 4, 2, 64, 16, "bf16", words=5)
+    want = b.run(max_queries=300).clone()
+    b.check(want)
+    for m in (1, 2, 20, 0):
+        b.check(b.run(max_queries=m), str(m))
+
+
 def test_offsets_beyond_32_bits():
     """Pages that lie more than 2^32 bytes apart: a cache in a buffer of 5 GB."""
     size, heads, page = 64, 2, 16

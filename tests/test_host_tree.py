@@ -244,6 +244,9 @@ def test_compact_refusals():
         (dict(caches=[cache(), cache(dv=other)]), "NT_ERR_SHAPE_MISMATCH", "one layout"),
         (dict(caches=[cache(dtype=F32)]), "NT_ERR_UNSUPPORTED", "dtype"),
         (dict(caches=[cache(dtype=E4M3)]), "NT_ERR_INVALID_ARG", "needs scales"),
+        (dict(caches=[cache(), cache(k=ADDRESS + 4096)]), "NT_ERR_INVALID_ARG", "listed twice"),
+        (dict(caches=[cache(), cache()]), "NT_ERR_INVALID_ARG", "listed twice"),
+        (dict(caches=[cache()], table=(1 << 23, 3), path=(1 << 23, 4)), "NT_ERR_UNSUPPORTED", "one launch"),
         (dict(caches=[cache()], table=None), "NT_ERR_INVALID_ARG", "null tensor descriptor"),
         (dict(caches=[cache()], table=(2, 3, 1)), "NT_ERR_SHAPE_MISMATCH", "2-D"),
         (dict(caches=[cache()], path=(3, 4)), "NT_ERR_SHAPE_MISMATCH", "differ in sequences"),
