@@ -132,14 +132,9 @@ __device__ __forceinline__ void cut_two(float a, float b, uint32_t *first, uint3
         x = a - widen_one<false>(*first, 0);
         y = b - widen_one<false>(*first, 1);
     }
-    if constexpr (SCALED) {
-        x = __builtin_fabsf(x) < INFINITY ? x : 0.f;
-        y = __builtin_fabsf(y) < INFINITY ? y : 0.f;
-    } else {
-        constexpr float least = BF16 ? 0x1p-126f : 0x1p-24f;
-        x = __builtin_amdgcn_fmed3f(x, a, least);
-        y = __builtin_amdgcn_fmed3f(y, b, least);
-    }
+    constexpr float least = SCALED ? 0.f : BF16 ? 0x1p-126f : 0x1p-24f;    // (SCALED, a weight times a scale: of an infinite one 0 or as much, never of the other sign)
+    x = __builtin_amdgcn_fmed3f(x, a, least);
+    y = __builtin_amdgcn_fmed3f(y, b, least);
     *rest = pack_two<BF16>(x, y);
 }
 

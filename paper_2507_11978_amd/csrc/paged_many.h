@@ -43,7 +43,8 @@ constexpr int many_resident(int kind, int size) { return size == 256 ? 1 : size 
 // FULL: rows of SIZE elements (the switched-off lanes of others cost 5 % where none is: 1024 queries x 8000 keys x 32/8 heads x 128 bf16 217 us, 228)
 // One tile: the rows of a sequence and key head from r0 on.
 // TREE: the new tokens are a tree's, what a row sees of them stands in its mask; [row_lo, row_hi) is what it sees of the past.  The tile's keys are given, and where its share of the
-// result goes, if it is one.  Weights multiply V as the sum of two 16-bit numbers (cut_two).  GROUPS: of wavefronts that share a block's keys, the rows being fewer by so much.
+// result goes, if it is one.  Weights multiply V as the sum of two 16-bit numbers (cut_two).  Over codes the keys' scales go into the exponent's multiplication, one instruction to a
+// weight less; with the one that cut_two saves 2 sequences of 64 tokens x 100000 to 131072 int8 keys x 32/8 heads x 128 bf16 take 460 us, 495 without.  GROUPS: of wavefronts that share a block's keys, the rows being fewer by so much.
 template <bool BF16, int KIND, int SIZE, bool FAST, bool FULL, bool TREE, int GROUPS>
 __device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const smem, const int b, const int h, const Sequence &seq, const int r0,
                                                 const int split, const KeyRange given, float *const share_ml, float *const share_o)
@@ -57,6 +58,8 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const 
     constexpr bool SPLIT = TREE || (VB && !BF16);                          // ... where that is not the queries', with weights in two parts: see rest_of
     constexpr bool SUMS = TREE || KIND != CACHE_SAME;                      // sums of the weights as they are, each lane of its keys
     constexpr int ROWS = kManyRows / GROUPS, ROW_WAVES = kManyWaves / GROUPS, JW = JB / GROUPS;     // 32-key parts of a block to a wavefront
+    constexpr bool LATE = TREE && KIND != CACHE_SAME;                      // keys' scales are kept times scale * log2(e), and multiplied in the exponent where no key is hidden
+    const float unit = LATE ? 1.f : g.scale_log2e;                         // (scores are then as they go into the exponent)
     static_assert(GROUPS == 1 || TREE, "built");
     constexpr int DEEP = 4;                                                // products that a fragment of K or V is read ahead of its own
     float *const scales = reinterpret_cast<float *>(smem + 4 * BLK);
@@ -231,7 +234,7 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const 
                 }
             }
             if constexpr (KIND != CACHE_SAME)
-                if (tid < 2 * KB) scales[copy * 2 * KB + tid] = sc;
+                if (tid < 2 * KB) scales[copy * 2 * KB + tid] = LATE && tid < KB ? sc * g.scale_log2e : sc;
             if (odd) flags[kb % 3] = 1;
         }
     };
@@ -275,21 +278,24 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const 
             if (i + DEEP < PRODUCTS) f[i % DEEP] = fragment(i + DEEP);
             __builtin_amdgcn_sched_barrier(0);
         }
-        if constexpr (KIND != CACHE_SAME) {
+        const bool hidden = base < all_lo || base + KB > all_hi;          // wavefront-uniform: from some row
+        auto key_scales = [&](int jb, int q) { return *reinterpret_cast<const float4v *>(&scales[copy * 2 * KB + 32 * (GROUPS > 1 ? jw + jb : jb) + 8 * q + 4 * hi]); };
+        auto scale_scores = [&] {
 #pragma unroll
             for (int jb = 0; jb < JW; ++jb)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const float4v k4 = *reinterpret_cast<const float4v *>(&scales[copy * 2 * KB + 32 * (GROUPS > 1 ? jw + jb : jb) + 8 * q + 4 * hi]);
+                    const float4v k4 = key_scales(jb, q);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) st[jb][4 * q + e] *= k4[e];
                 }
-        }
-        const bool hidden = base < all_lo || base + KB > all_hi;          // wavefront-uniform: from some row
+        };
+        const bool late = LATE && !hidden && !pending;                     // wavefront-uniform
+        if (KIND != CACHE_SAME && !late) scale_scores();
         uint64_t vis = ~0ull;                                              // (TREE: which keys of the wavefront's part of the block the row sees, from key 4 hi on)
         if constexpr (TREE) {
             if (hidden) {
-                const float out = g.scale_log2e >= 0.f ? -INFINITY : INFINITY;
+                const float out = unit >= 0.f ? -INFINITY : INFINITY;
                 vis = row_bits(base + 32 * jw) >> (4 * hi);
 #pragma unroll
                 for (int jb = 0; jb < JW; ++jb)
@@ -306,7 +312,8 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const 
         }
         // ---- weights and their sum
         float rs;
-        auto exponentials = [&](const float m) {
+        auto exponentials = [&](const float m, auto scaled) {              // scaled: the scores are
+            constexpr bool SCALED = decltype(scaled)::value;
             float sum = 0.f;
 #pragma unroll
             for (int jb = 0; jb < JW; ++jb)
@@ -315,8 +322,10 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const 
 #pragma unroll
                     for (int q = 0; q < 2; ++q) {
                         float p[4];
+                        float4v by{unit, unit, unit, unit};
+                        if constexpr (!SCALED) by = key_scales(jb, 2 * s2 + q);
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[jb][8 * s2 + 4 * q + e], g.scale_log2e, -m));
+                        for (int e = 0; e < 4; ++e) p[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(st[jb][8 * s2 + 4 * q + e], by[e], -m));
                         if constexpr (SUMS) sum += (p[0] + p[1]) + (p[2] + p[3]);
                         if constexpr (KIND != CACHE_SAME) {
                             const float4v v4 = *reinterpret_cast<const float4v *>(&scales[copy * 2 * KB + KB + 32 * (GROUPS > 1 ? jw + jb : jb) + 16 * s2 + 8 * q + 4 * hi]);
@@ -356,14 +365,20 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const 
         // A row's weights, sum and reference depend on that row alone, also where a neighbour in the wavefront needs its reference raised.
         bool accept = false;
         if (!pending) {
-            exponentials(m_ref);
+            if constexpr (LATE) {
+                if (late) exponentials(m_ref, std::false_type{});
+                else exponentials(m_ref, std::true_type{});
+            } else {
+                exponentials(m_ref, std::true_type{});
+            }
             if constexpr (!SUMS) rs = matrix_sum(false);
             accept = __all(rs < 32768.f);
         }
         if (!accept) {                                                     // wavefront-uniform: a row without reference, or a score far above M
+            if (late) scale_scores();
             bool keep = false;                                             // this row's reference is close enough
             if (__any(m_ref != -INFINITY)) {
-                exponentials(m_ref == -INFINITY ? 0.f : m_ref);
+                exponentials(m_ref == -INFINITY ? 0.f : m_ref, std::true_type{});
                 if constexpr (!SUMS) rs = matrix_sum(true);
                 keep = m_ref != -INFINITY && rs < 32768.f;
                 if constexpr (SUMS) {
@@ -375,11 +390,11 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const 
 #pragma unroll
             for (int jb = 0; jb < JW; ++jb)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) mx = fmaxf(mx, st[jb][v] * g.scale_log2e);
+                for (int v = 0; v < 16; ++v) mx = fmaxf(mx, st[jb][v] * unit);
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
             const float m_new = keep ? m_ref : fmaxf(m_ref, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
             const float alpha = __builtin_amdgcn_exp2f(m_ref - m_use);
-            exponentials(m_use);
+            exponentials(m_use, std::true_type{});
             if constexpr (!SUMS) rs = matrix_sum(true);
             l_run *= alpha;
 #pragma unroll
