@@ -19,7 +19,7 @@
 // e4m3 290 to 297, int8 304 to 310 (each lane widens 64 elements of a block and scales 64 scores and weights), fp16 over them 365 and 376.  A block of 64 keys is
 // 32 matrix instructions of 32 cycles and 4 of 16 to a wavefront beside 32 exponentials, the multiplications and packs that feed them; the matrix pipe is busy for
 // 44 % of the cycles, LDS has no conflicts.  Two wavefronts to a SIMD (128; three at 64) are what the registers allow, and where both weigh their blocks the pipe
-// waits.  Tried: the next block's products between this block's exponentials (K two blocks ahead, two sets of scores): 629 us with all 256 registers, but 7.5 %
+// waits.  Tried: priority for the wavefronts that multiply: no difference; the next block's products between this block's exponentials (K two blocks ahead, two sets of scores): 629 us with all 256 registers, but 7.5 %
 // slower at head size 64 and half again as long where registers ran out; blocks of 32 keys: 775.  Hidden keys of codes told by their weight in every block, not
 // by position in those that have any: 8 % longer.
 #pragma once
@@ -44,7 +44,8 @@ constexpr int many_resident(int kind, int size) { return size == 256 ? 1 : size 
 // One tile: the rows of a sequence and key head from r0 on.
 // TREE: the new tokens are a tree's, what a row sees of them stands in its mask; [row_lo, row_hi) is what it sees of the past.  The tile's keys are given, and where its share of the
 // result goes, if it is one.  Weights multiply V as the sum of two 16-bit numbers (cut_two).  Over codes the keys' scales go into the exponent's multiplication, one instruction to a
-// weight less; with the one that cut_two saves 2 sequences of 64 tokens x 100000 to 131072 int8 keys x 32/8 heads x 128 bf16 take 460 us, 495 without.  GROUPS: of wavefronts that share a block's keys, the rows being fewer by so much.
+// weight less; with the one that cut_two saves 2 sequences of 64 tokens x 100000 to 131072 int8 keys x 32/8 heads x 128 bf16 take 460 us, 495 without.  452 where blocks that are whole are
+// not checked key by key and codes are known to come from global memory (without trees, 2048 queries of 32/8 heads x 128 bf16 over 18500 e4m3 keys 692, 711 without; 4 x 1024 x 48 heads x 64 f16 91.6, 95.7).  GROUPS: of wavefronts that share a block's keys, the rows being fewer by so much.
 template <bool BF16, int KIND, int SIZE, bool FAST, bool FULL, bool TREE, int GROUPS>
 __device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const smem, const int b, const int h, const Sequence &seq, const int r0,
                                                 const int split, const KeyRange given, float *const share_ml, float *const share_o)
@@ -145,7 +146,9 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const 
         }
         auto of_lane = [&](int l) {
             const uint64_t p = reinterpret_cast<uint64_t>(address[0][0]);
-            return reinterpret_cast<const char *>((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)p, l) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(p >> 32), l) << 32);
+            // (of global memory: a load that might be of LDS is waited for by every read of LDS behind it)
+            return (const char *)reinterpret_cast<const __attribute__((address_space(1))) char *>((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)p, l) |
+                                                                                                  (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(p >> 32), l) << 32);
         };
         if constexpr (DMA) {
             const uint32_t to = lds0 + copy * BLK + (uint32_t)(wave * (RSTEP / 4) * SIZE * 2);
@@ -206,6 +209,8 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const 
             }
         } else {
             bool odd = false;
+            // (FAST) all keys of the block have pages and are in the range: wavefront-uniform
+            const bool whole = FAST && named == (1u << PER) - 1 && !hidden && kb * KB >= keys.lo && kb * KB + KB <= keys.hi;
 #pragma unroll
             for (int u = 0; u < PER; ++u) {
                 const uint32_t r = u * RSTEP + row0;
@@ -225,9 +230,11 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const 
                         v = widen8<VB, KIND>(u32x2{vr[u][0], vr[u][1]});
                     }
                     if (!FULL && EPL * ch >= g.D) k = v = u32x4{0, 0, 0, 0};
-                    k = page ? k : u32x4{kNanPair, kNanPair, kNanPair, kNanPair};
-                    v = good ? v : u32x4{0, 0, 0, 0};
-                    if (hidden) odd = odd | any_not_finite<VB>(v);
+                    if (!whole) {
+                        k = page ? k : u32x4{kNanPair, kNanPair, kNanPair, kNanPair};
+                        v = good ? v : u32x4{0, 0, 0, 0};
+                        if (hidden) odd = odd | any_not_finite<VB>(v);
+                    }
                     const uint32_t at = lds_at<SIZE>(r, EPL / 8 * ch + half);
                     lds_write16(smem, copy * BLK + at, k);
                     lds_write16(smem, (2 + copy) * BLK + at, v);

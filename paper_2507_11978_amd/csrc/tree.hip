@@ -42,30 +42,36 @@ __global__ __launch_bounds__(256) void tree_masks_kernel(const MasksArgs g)
     const int b = blockIdx.x;
     const int32_t first = clamp_i32(g.starts[b], 0, g.T), count = clamp_i32(g.starts[b + 1], first, g.T) - first;
     const int32_t *parents = g.parents + first;
-    for (int i = threadIdx.x; i < count && i < kParentsHere; i += blockDim.x) near[i] = parents[i];
+    if (count <= kParentsHere)
+        for (int i = threadIdx.x; i < count; i += blockDim.x) near[i] = parents[i];
     __syncthreads();
-    for (int32_t i = threadIdx.x; i < count; i += blockDim.x) {
-        uint64_t *mask = g.masks + (int64_t)(first + i) * g.m_st, bits = 0;
-        int32_t depth = 0, word = g.words - 1;
-        for (int32_t j = i;; ++depth) {
-            if (!g.window || depth < g.window) {
-                for (; word > (j >> 6); --word) {
-                    mask[word] = bits;
-                    bits = 0;
+    // (from LDS or from memory, not from either: a load that may be of both is as slow as the slower)
+    const auto walks = [&](const int32_t *from) __attribute__((always_inline)) {
+        for (int32_t i = threadIdx.x; i < count; i += blockDim.x) {
+            uint64_t *mask = g.masks + (int64_t)(first + i) * g.m_st, bits = 0;
+            int32_t depth = 0, word = g.words - 1;
+            for (int32_t j = i;; ++depth) {
+                if (!g.window || depth < g.window) {
+                    for (; word > (j >> 6); --word) {
+                        mask[word] = bits;
+                        bits = 0;
+                    }
+                    if (word == (j >> 6)) bits |= 1ull << (j & 63);        // (not where the masks have too few words)
                 }
-                if (word == (j >> 6)) bits |= 1ull << (j & 63);            // (not where the masks have too few words)
+                const int32_t p = from[j];
+                if (p < 0 || p >= j) break;
+                j = p;
             }
-            const int32_t p = j < kParentsHere ? near[j] : parents[j];
-            if (p < 0 || p >= j) break;
-            j = p;
+            for (; word >= 0; --word) {
+                mask[word] = bits;
+                bits = 0;
+            }
+            g.depths[first + i] = depth;
+            if (g.positions) g.positions[first + i] = g.lengths[b] - count + depth;
         }
-        for (; word >= 0; --word) {
-            mask[word] = bits;
-            bits = 0;
-        }
-        g.depths[first + i] = depth;
-        if (g.positions) g.positions[first + i] = g.lengths[b] - count + depth;
-    }
+    };
+    if (count <= kParentsHere) walks(near);
+    else walks(parents);
 }
 
 nt_status launch_tree_masks(const int32_t *parents, const int32_t *starts, int64_t sequences, uint64_t *masks, const nt_tensor_desc *dm, int32_t *depths,
