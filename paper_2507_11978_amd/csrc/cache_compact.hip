@@ -5,7 +5,8 @@
 // 8 elements of one head of one cache and takes the tokens in order, so that no other lane's reads matter to it: loads of several tokens go out together, ahead of
 // their stores, and none is behind a store to the place that it reads (path[j] > path[k] >= k).
 //
-// Bound by memory, and where few tokens move by the chain path, table, row, store.
+// Bound by memory, and where few tokens move by the chain path, table, row, store: 64 sequences of 1 to 32 tokens, 16 layers of 8 heads x 128 bf16 7.0 us for 20 MB (2.9 TB/s), one
+// sequence, 4 layers 3.0.  (Token after token, with a branch around what is in place already, 21 us.)
 #include "paged.h"
 
 namespace nt {

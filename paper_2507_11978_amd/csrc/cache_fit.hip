@@ -6,6 +6,9 @@
 //
 // One workgroup does it, a sequence to a thread, 1024 at a time; the pages that move are dealt out to all threads (a bisection tells whose each is), so that a long prompt's
 // pages are not one thread's.  Then a thread to a token.
+//
+// Bound by its chain, not by bytes: lengths, scan, stack or table, starts, page, slot, one waiting for the other.  256 sequences that get a token each 5.9 us; 96 of them, a third
+// new prompts and a third that end, 51000 tokens 6.2 us and 3.6 of the second launch (16.2 called).  Three scans one after the other instead of one took 2.6 us more.
 #include "gemm_fast.h"
 #include "kernels.h"
 #include "paged_index.h"

@@ -9,14 +9,14 @@
 //
 // Weights are rounded to 16 bits once, and over 16-bit caches their sum is that of the rounded ones.  In two parts, as in paged_few.h, they would cost a second set of
 // products where products are the bound (1024 queries x 8000 keys x 32/8 heads x 128 bf16 212 us, 276 with two; 4 x 1024 x 48 heads x 64 f16 64, 98).  fp16 queries
-// over codes have no choice, see rest_of (20 us of the 365 that 1024 x 8000 e4m3 take).
+// over codes have no choice, see rest_of (20 us of the 356 that 1024 x 8000 e4m3 take).
 //
 // FAST (rows at addresses that are multiples of 16 bytes, and pages that hold the 2 to 16 rows that a wavefront moves with one load or a multiple of
 // them, so that these lie on one page): the table is read and the addresses are made by one lane for all.  A 16-bit cache then travels straight into
 // LDS, one block ahead, codes through registers, 16 at a time.  Other caches: 8 elements to a lane through registers, every lane with an address of its own.
 //
 // Measured: 2048 queries of 32/8 heads x 128 bf16 over 18500 keys 620 to 650 us = 0.90 to 0.94 PFLOP/s (a large matrix product reaches 1.18), 1024 queries x 8000 211, over
-// e4m3 290 to 297, int8 304 to 310 (each lane widens 64 elements of a block and scales 64 scores and weights), fp16 over them 365 and 376.  A block of 64 keys is
+// e4m3 277 to 281, int8 290 (each lane widens 64 elements of a block and scales 64 scores and weights), fp16 over them 356 and 353.  A block of 64 keys is
 // 32 matrix instructions of 32 cycles and 4 of 16 to a wavefront beside 32 exponentials, the multiplications and packs that feed them; the matrix pipe is busy for
 // 44 % of the cycles, LDS has no conflicts.  Two wavefronts to a SIMD (128; three at 64) are what the registers allow, and where both weigh their blocks the pipe
 // waits.  Tried: priority for the wavefronts that multiply: no difference; the next block's products between this block's exponentials (K two blocks ahead, two sets of scores): 629 us with all 256 registers, but 7.5 %
