@@ -417,8 +417,8 @@ nt_status nt_tree_masks(const int32_t *parents, const int32_t *starts, int64_t s
  * lengths[b] - n + k, those whose bit k is set in its row of masks (as nt_tree_masks makes them; any bits will do, a token need not see itself; bits of
  * numbers from n on mean nothing).  window > 0: of the past the positions j > lengths[b] - n + depths[t] - window (depths[t] is taken as 0 to n - 1; needed with a window only).
  * What a token does not see has no part in its result; one that sees nothing, or nothing with a score above -inf, gets zeros, one that sees a position without a page NaN.
- * Scores, weights' sums and accumulators are fp32; what multiplies V is the weight as the sum of two numbers of `dtype` (bf16 over codes), off by 2^-16 of it at most (fp16: 2^-22,
- * or 2^-24 of a weight of 1).  max_queries (the most new tokens of a sequence, 0: not known) chooses how rows are dealt out; one that is too low costs time and is not an
+ * Scores, weights' sums and accumulators are fp32; what multiplies V is the weight as the sum of two numbers of `dtype` (bf16 over codes), off by 2^-16 of it at most (fp16: 2^-22
+ * of it, or 2^-31 of the row's largest).  max_queries (the most new tokens of a sequence, 0: not known) chooses how rows are dealt out; one that is too low costs time and is not an
  * error.  The keys are dealt out by the lengths, which only the device needs to know: max_length is checked and not used.
  * Memory: results of keys that are shared out (up to 1024 sequences) pass through the library's workspace under the rules given at nt_conv2d_implicit, and are added in the order
  * of the keys; without room for them every sequence's keys are one program's. */

@@ -116,9 +116,11 @@ __device__ __forceinline__ uint32_t rest_of(uint32_t packed, float a, float b)
     return pack_two<BF16>(x, y);
 }
 
-// Two weights as the sums of two 16-bit numbers each, the first cut off, so that the rest is not negative: as long as it is more than 0 an infinity that it multiplies stays
-// one, which the rest of a rounded weight, of either sign or 0, makes NaN.  A rest of 0 becomes the type's smallest normal number (fp16: smallest of all, 2^-24 of a weight of 1);
-// that of a weight of 0 stays 0.  Off by 2^-16 of the weight in bf16, 2^-22 or 2^-24 of a weight of 1 in fp16.  SCALED: as above; values then are codes, no infinities.
+// Two weights as the sums of two 16-bit numbers each, the first cut off, so that the rest is not negative: as long as both are more than 0 an infinity that they multiply stays
+// one, which the rest of a rounded weight, of either sign or 0, makes NaN.  A rest below the type's smallest normal number (fp16: smallest of all, 2^-24) becomes that, and fp16 weights
+// below 2^-24 are taken as 2^-24; of a weight of 0 both stay 0.  Off by 2^-16 of the weight in bf16, 2^-22 of it or 2^-24 in fp16, 2^-23 where it is below 2^-24.  These are to one side,
+// and would add up over the keys (131072 beside one that weighs as much as twice all of them: 1e-3 of the result with a largest weight of 1): fp16 weights are such that a row's
+// largest is 2^8 or more, 2^-24 then 2^-32 of it or less.  SCALED: as above; values then are codes, no infinities.
 template <bool BF16, bool SCALED>
 __device__ __forceinline__ void cut_two(float a, float b, uint32_t *first, uint32_t *rest)
 {
@@ -128,6 +130,10 @@ __device__ __forceinline__ void cut_two(float a, float b, uint32_t *first, uint3
         x = a - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, a) & 0xffff0000u);
         y = b - __builtin_bit_cast(float, __builtin_bit_cast(uint32_t, b) & 0xffff0000u);
     } else {
+        if constexpr (!SCALED) {                                           // (2^100 a is above 2^-24 for every weight that is not 0)
+            a = __builtin_amdgcn_fmed3f(a, a * 0x1p100f, 0x1p-24f);
+            b = __builtin_amdgcn_fmed3f(b, b * 0x1p100f, 0x1p-24f);
+        }
         *first = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(a, b));
         x = a - widen_one<false>(*first, 0);
         y = b - widen_one<false>(*first, 1);

@@ -62,6 +62,8 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const 
     constexpr bool LATE = TREE && KIND != CACHE_SAME;                      // keys' scales are kept times scale * log2(e), and multiplied in the exponent where no key is hidden
     const float unit = LATE ? 1.f : g.scale_log2e;                         // (scores are then as they go into the exponent)
     static_assert(GROUPS == 1 || TREE, "built");
+    // fp16 weights in two parts: the reference lies 8 binary places below the largest score (cut_two); a block's weights, which are summed up to 2^15, then still pass it by 2 to 7 places
+    constexpr float BELOW = TREE && !VB ? 8.f : 0.f;
     constexpr int DEEP = 4;                                                // products that a fragment of K or V is read ahead of its own
     float *const scales = reinterpret_cast<float *>(smem + 4 * BLK);
     int *const flags = reinterpret_cast<int *>(scales + 4 * KB);
@@ -369,7 +371,8 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const 
             }
             return apart && l32 >= 16 ? sum[1][0] : sum[0][0];
         };
-        // A row's weights, sum and reference depend on that row alone, also where a neighbour in the wavefront needs its reference raised.
+        // A row's weights, sum and reference depend on that row alone, also where a neighbour in the wavefront needs its reference raised (LATE: but for a rounding of the scores,
+        // which that multiplies by the keys' scales ahead of the exponent).
         bool accept = false;
         if (!pending) {
             if constexpr (LATE) {
@@ -399,7 +402,7 @@ __device__ __forceinline__ void paged_many_tile(const PagedArgs &g, char *const 
 #pragma unroll
                 for (int v = 0; v < 16; ++v) mx = fmaxf(mx, st[jb][v] * unit);
             mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-            const float m_new = keep ? m_ref : fmaxf(m_ref, mx), m_use = m_new == -INFINITY ? 0.f : m_new;
+            const float m_new = keep ? m_ref : fmaxf(m_ref, mx - BELOW), m_use = m_new == -INFINITY ? 0.f : m_new;
             const float alpha = __builtin_amdgcn_exp2f(m_ref - m_use);
             exponentials(m_use, std::true_type{});
             if constexpr (!SUMS) rs = matrix_sum(true);

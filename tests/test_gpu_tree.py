@@ -839,3 +839,38 @@ def test_two_streams():
     torch.cuda.synchronize()
     assert all(torch.equal(x, w) for g, w in zip(got, want) for x in g)
     assert all(x == w for g, w in zip(got_v, want_v) for x in g)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+def test_small_weights_are_not_off_to_one_side(dt):
+    """One key with 70 % of a row, 131072 others of some 2^-18 each, all of one program (more sequences than are dealt out): a weight's error has no side that adds up over the keys.
+
+    V is 1, so that what the scores are off by cancels.  A weight multiplies V as two numbers, rounded to nearest or raised by 2^-32 of the largest (2^-16 of itself in bf16): n 2^-32, or 2^-17
+    on its side.  fp32 sums of n numbers, their roundings of either sign: 6 sqrt(n) 2^-24 for six times their spread.  The result's rounding: half a step."""
+    n, size = 131072, 64
+    b = Trees([(1, n)] + [(0, 0)] * 1024, 1, 1, size, 1024, dt, seed=7)
+    q, first = b.q[0, 0].double(), int(b.table[0, 0])
+    k = b.c[0][torch.tensor(b.table[0, :n // 1024], device="cuda")].double().view(n, size)
+    rest = torch.exp((k[1:] @ q) / 8).sum().item()
+    b.c[0][first, 0, 0] = (q * (np.log(rest * 0.7 / 0.3) * 8 / (q @ q).item())).to(TORCH[dt])
+    b.c[1].fill_(1.0)
+    got = f64(b.run(max_queries=1))
+    h = torch.finfo(TORCH[dt]).eps / 2
+    assert np.abs(got - 1).max() <= h + 6 * n ** 0.5 * 2.0 ** -24 + (n * 2.0 ** -32 if dt == "f16" else 2.0 ** -17)
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("size", [64, 128, 256])
+def test_infinities_with_small_weights(dt, size):
+    """An infinity that every row sees at a weight of e^-20 of the largest, in the same block, stays one."""
+    for bad in (float("inf"), -float("inf")):
+        b = Trees([(5, 400), (3, 90)], 2, 1, size, 16, dt, seed=2)
+        b.q.fill_(1.0)
+        b.c[0][int(b.table[0, 0]), 3] = 20 * size ** -0.5
+        want = b.run().clone()
+        b.check(want)
+        b.c[1][int(b.table[0, 1]), 4, 0, 7] = bad
+        got = b.run()
+        hit = torch.zeros_like(got, dtype=torch.bool)
+        hit[:5, :, 7] = True
+        assert torch.equal(got[~hit], want[~hit]) and (got[hit] == bad).all()
