@@ -260,7 +260,7 @@ __device__ __forceinline__ double group_sum(double v, double *scratch)
 }
 
 // The first element of [lo, hi) whose weight brings the sum, `before` ahead of lo, above `goal`; rounding may leave none: then the last with a weight, -1 if there is
-// none.  A sixteenth of the range to a wavefront until it is short.
+// none.  (What has no weight is never chosen: sums of the same numbers in another order may put `before` itself above the goal.)  A sixteenth of the range to a wavefront until it is short.
 template <typename T, bool DRAFT>
 __device__ int32_t find_above(const Left<T, DRAFT> &left, int32_t lo, int32_t hi, double before, double goal, double *scratch, int32_t *found)
 {
@@ -282,7 +282,7 @@ __device__ int32_t find_above(const Left<T, DRAFT> &left, int32_t lo, int32_t hi
                 last = w;
                 at_last = run;
             }
-            if (chosen < 0 && next > goal) {
+            if (chosen < 0 && scratch[w] > 0.0 && next > goal) {
                 chosen = w;
                 at_chosen = run;
             }
@@ -476,7 +476,7 @@ struct Chunks {
         double run = upto - mine, at_above = 0.0, at_last = 0.0;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            if (above < 0 && run + v[i] > goal) {
+            if (above < 0 && v[i] > 0.0 && run + v[i] > goal) {
                 above = i;
                 at_above = run;
             }

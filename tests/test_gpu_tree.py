@@ -874,3 +874,46 @@ def test_infinities_with_small_weights(dt, size):
         hit = torch.zeros_like(got, dtype=torch.bool)
         hit[:5, :, 7] = True
         assert torch.equal(got[~hit], want[~hit]) and (got[hit] == bad).all()
+
+
+def sums_at_a_border(g, tiny):
+    """256 sums of chunks, four to a lane: added lane by lane and then by a scan, what is ahead of some lane comes out above the run to the end of the lane before it, and half of all lies between.
+    `tiny`: of that lane's first chunk."""
+    def scanned(v):
+        mine = ((v[:, 0] + v[:, 1]) + v[:, 2]) + v[:, 3]
+        upto, d = mine.copy(), 1
+        while d < 64:
+            upto[d:] = upto[d:] + upto[:-d]
+            d *= 2
+        return mine, upto
+    while True:
+        v = np.zeros((64, 4))
+        lane = int(g.integers(3, 50))
+        v[:lane] = np.exp2(g.uniform(-40, 0, (lane, 4))).astype(np.float32)
+        v[lane, 0] = tiny
+        mine, upto = scanned(v)
+        run = upto[lane - 1] - mine[lane - 1]
+        for x in v[lane - 1]:
+            run = run + x
+        left = run
+        for i in range(3):                                                    # as much again, in three numbers of 32 bits
+            v[60, i] = np.float32(left) if np.float32(left) <= left else np.nextafter(np.float32(left), np.float32(0))
+            left -= v[60, i]
+        if run <= 0.5 * scanned(v)[1][63] < upto[lane] - mine[lane]:
+            return v.reshape(-1)
+
+
+@pytest.mark.parametrize("V,tiny", [(256 * 1024, 0.0), (256 * 8192, 2.0 ** -90)])
+def test_goals_between_two_sums(V, tiny):
+    """The next token has a weight also where the random number falls between two sums of the same numbers, added in another order."""
+    g, V = np.random.default_rng(3), V
+    d = Drafts([[-1]], V, "f32", False)
+    d.r.fill_(0.5)
+    for _ in range(20):
+        w = np.zeros((256, V // 256))
+        w[:, -1] = sums_at_a_border(g, tiny)
+        w = w.reshape(-1)
+        d.target.copy_(torch.from_numpy(w)[None])
+        token = d.run()[2][0]
+        upto = np.cumsum(w)
+        assert w[token] > 0 and upto[token] - w[token] <= upto[-1] * (0.5 + 1e-12) and upto[token] >= upto[-1] * (0.5 - 1e-12)
