@@ -117,10 +117,26 @@ struct Walk {
     int32_t node, accepted, tried, at;                                     // tokens before `at` have been passed
 };
 
+// A sum m and 1 / m, rounded to nearest; 0 and 0 where m is 0
+struct Sum {
+    double m, inverse;
+};
+__device__ __forceinline__ Sum sum_and_inverse(double m) { return Sum{m, m > 0.0 ? 1.0 / m : 0.0}; }
+
+// w / m, rounded to nearest, 0 where m is 0.  w times the inverse is within two last places; one correction by the remainder makes it one of the two neighbours, from which the
+// next gives the nearest (Markstein's theorem: an inverse rounded to nearest, a remainder without rounding).  64 trees of 24, 128000 words 90.5 us so, 109 with divisions, each of which
+// finds the inverse anew, 87 with one correction.  81 with products by the inverse alone: but then w / m that is q leaves something or not by how the inverse was rounded.
+__device__ __forceinline__ double quotient(double w, const Sum &s)
+{
+    double q = w * s.inverse;
+    q = __builtin_fma(__builtin_fma(-q, s.m, w), s.inverse, q);
+    return __builtin_fma(__builtin_fma(-q, s.m, w), s.inverse, q);
+}
+
 struct VerifyState {
     Walk walk;
     int32_t done, summed;                                                  // the walk has ended; the sums are of where it did
-    double over[kMostTried];
+    Sum over[kMostTried];
     int64_t gone[kMostTried];
 };
 
@@ -146,7 +162,7 @@ struct Left {
         T v[N];
     };
     const T *p, *q;
-    const double *over;                                                    // (DRAFT) 1 / m before rejection number j, 0 where m was 0
+    const Sum *over;                                                       // (DRAFT) m before rejection number j
     const int64_t *gone;                                                   // (not DRAFT) tokens whose weight is 0
     int32_t tried;
 
@@ -161,7 +177,7 @@ struct Left {
             const double q1 = weight_of(qv);
             w = __builtin_fmax(w - q1, 0.0);
             if constexpr (FEW != 1)
-                for (int j = 1; j < tried; ++j) w = __builtin_fmax(w * over[j] - q1, 0.0);
+                for (int j = 1; j < tried; ++j) w = __builtin_fmax(quotient(w, over[j]) - q1, 0.0);
         } else if constexpr (FEW == ANY) {
             for (int j = 0; j < tried; ++j) w = gone[j] == t ? 0.0 : w;
         }
@@ -343,7 +359,7 @@ __device__ int32_t find_above(const Left<T, DRAFT> &left, int32_t lo, int32_t hi
 // The walk, which every wavefront makes for itself (a token to a lane, its numbers loaded ahead of it).  m: after the `tried` rejections, if known.  False: m is needed and not known
 // (SELF: worked out here).
 template <typename T, bool DRAFT, bool SELF, int THREADS>
-__device__ __forceinline__ bool walk_tree(const VerifyArgs &g, const int32_t first, const int32_t count, int32_t *path, Walk &s, double m, bool known, double *over, int64_t *gone,
+__device__ __forceinline__ bool walk_tree(const VerifyArgs &g, const int32_t first, const int32_t count, int32_t *path, Walk &s, double m, bool known, Sum *over, int64_t *gone,
                                           double *scratch)
 {
     const int tid = threadIdx.x, lane = tid & 63;
@@ -379,7 +395,7 @@ __device__ __forceinline__ bool walk_tree(const VerifyArgs &g, const int32_t fir
             } else {
                 __syncthreads();                                           // (all wavefronts are here: they walk alike; what is written below may still be read)
                 if (tid == 0) {
-                    if (DRAFT) over[s.tried] = m > 0.0 ? 1.0 / m : 0.0;
+                    if (DRAFT) over[s.tried] = sum_and_inverse(m);
                     else gone[s.tried] = xl;
                 }
                 __syncthreads();
@@ -425,7 +441,8 @@ __device__ __forceinline__ int32_t count_of(const VerifyArgs &g, int b) { return
 template <typename T, bool DRAFT>
 __global__ __launch_bounds__(kVerifyThreads) void verify_tree_kernel(const VerifyArgs g)
 {
-    __shared__ double scratch[kVerifyWaves], over[kMostTried];
+    __shared__ double scratch[kVerifyWaves];
+    __shared__ Sum over[kMostTried];
     __shared__ int64_t gone[kMostTried];
     __shared__ int32_t found[2];
     const int b = blockIdx.x;
@@ -498,7 +515,8 @@ template <typename T, bool DRAFT, bool FIRST, bool LAST>
 __global__ __launch_bounds__(LAST ? kVerifyThreads : 64) void verify_walk_kernel(const VerifyArgs g)
 {
     constexpr int THREADS = LAST ? kVerifyThreads : 64;
-    __shared__ double scratch[kVerifyWaves], over[kMostTried];
+    __shared__ double scratch[kVerifyWaves];
+    __shared__ Sum over[kMostTried];
     __shared__ int64_t gone[kMostTried];
     const int b = blockIdx.x, tid = threadIdx.x;
     const int32_t first = first_of(g, b), count = count_of(g, b);

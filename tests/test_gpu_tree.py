@@ -917,3 +917,19 @@ def test_goals_between_two_sums(V, tiny):
         token = d.run()[2][0]
         upto = np.cumsum(w)
         assert w[token] > 0 and upto[token] - w[token] <= upto[-1] * (0.5 + 1e-12) and upto[token] >= upto[-1] * (0.5 - 1e-12)
+
+
+@pytest.mark.parametrize("V", [4, 20001, 200003])
+def test_what_is_left_is_a_quotient(V):
+    """w / m - q where w / m is exactly q: nothing is left, and the next token is the target's.  (1 / m, rounded, is above it: with the product something would be left.)"""
+    d = Drafts([[-1, 0, 0] + [1] * 7] * 2, V, "f32", True)
+    d.target.fill_(0)
+    d.draft.fill_(0)
+    q, m = 3 / 32, 91 / 2 ** 14
+    assert q * m * (1 / m) > q
+    d.draft[:, 0], d.draft[:, 1], d.draft[:, 2], d.draft[:, 3] = q, 1 - q, 0.5, 0.75
+    d.target[:, 0], d.target[:, 1], d.target[:, 3] = q + q * m, (1 - q) + (1 - q) * m, 0.5
+    d.ids.fill_(2)
+    d.r[:] = torch.tensor([0.99, 0.1])
+    want = d.check()
+    assert want[1:] == ([1, 1], [3, 1])
