@@ -72,7 +72,7 @@ def law(logits, temperature):
 
 
 def generate(target, draft, prompts, new, depth=4, branch=2, kind="same", page_size=16, temperature=1.0, seed=0):
-    """At least `new` tokens behind each prompt; returns the texts, the tokens that stood in each step [steps, sequences], and the seconds of the steps."""
+    """At least `new` tokens behind each prompt; returns the texts, the tokens that stood in each step [steps, sequences] (0: the sequence waited), and the seconds of the steps."""
     B, dev = len(prompts), target.device
     parents = tree(depth, branch)
     n = len(parents)
@@ -124,8 +124,13 @@ def generate(target, draft, prompts, new, depth=4, branch=2, kind="same", page_s
         slots, _, _ = t.grow(each, B * n)
         rows = law(t(ids.flatten(), slots, positions, starts, masks, n), temperature)
         following = torch.empty(B, dtype=torch.int64, device=dev)
+        full = t.lengths + (depth + 1) > most                               # no room for another tree behind this one: has its new tokens, and waits for the slower ones
         u, r = torch.rand(B * n, generator=gen, device=dev), torch.rand(B, generator=gen, device=dev)
         nt.verify_tree(rows, drafts, ids.flatten(), all_parents, starts, u, r, path, accepted, following, t.lengths, t.lengths)
+        t.lengths.sub_(accepted * full)
+        accepted.masked_fill_(full, 0)
+        path.masked_fill_(full[:, None], -1)
+        following = torch.where(full, root, following)
         d.lengths.copy_(t.lengths)
         for s in both:
             nt.cache_compact([c if c[2] is not None else c[:2] for c in s.model.cache], s.table, s.lengths, path, accepted)
@@ -139,7 +144,8 @@ def generate(target, draft, prompts, new, depth=4, branch=2, kind="same", page_s
     for p, ids, following in steps:
         stood.append((p >= 0).sum(1).tolist())
         for b in range(B):
-            texts[b] += [ids[b, i].item() for i in p[b].tolist() if i > 0] + [following[b].item()]
+            if stood[-1][b]:
+                texts[b] += [ids[b, i].item() for i in p[b].tolist() if i > 0] + [following[b].item()]
     return texts, stood, seconds
 
 
