@@ -933,3 +933,36 @@ def test_what_is_left_is_a_quotient(V):
     d.r[:] = torch.tensor([0.99, 0.1])
     want = d.check()
     assert want[1:] == ([1, 1], [3, 1])
+
+
+def test_more_streams_than_workspaces():
+    """Calls of five streams, none waited for by the host: the attention's shares (34 MB) meet in the one large piece of the workspace, the verification's states and sums in three small ones."""
+    bs = [Trees([(9, 3500), (3, 2000 + 100 * s)], 4, 1, 128, 16, "f16", seed=s) for s in range(5)]
+    ds = [Drafts([random_tree(9, np.random.default_rng(s))] * 3, 50000, seed=s) for s in range(5)]
+    calls = []
+    for b, d in zip(bs, ds):
+        a, ids, parents, starts, u, r, lengths = b.args(), d.ids.cuda(), i32(d.parents), i32(d.starts), d.u.cuda(), d.r.cuda(), i32(d.lengths)
+
+        def call(out, path, accepted, following, after, a=a, d=d, v=(ids, parents, starts, u, r), lengths=lengths):
+            nt.sdpa_paged_tree(*a[:7], out, *a[8:], max_queries=9)
+            nt.verify_tree(d.target, d.draft, *v, path, accepted, following, lengths, after)
+        calls.append(call)
+
+    def outputs(b):
+        return torch.full_like(b.q, -5.0), i32([[-7] * 6] * 3), i32([-7] * 3), i64([-7] * 3), i32([-7] * 3)
+    want, got = [outputs(b) for b in bs], [[outputs(b) for _ in range(20)] for b in bs]
+    for call, o in zip(calls, want):
+        call(*o)
+        torch.cuda.synchronize()
+    for b, d, o in zip(bs, ds, want):
+        b.check(o[0])
+        assert (o[1].tolist(), o[2].tolist(), o[3].tolist(), o[4].tolist()) == d.run()
+    streams = [torch.cuda.Stream() for _ in bs]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for call, o, s in zip(calls, got, streams):
+            with torch.cuda.stream(s):
+                call(*o[i])
+    torch.cuda.synchronize()
+    for w, runs in zip(want, got):
+        assert all(torch.equal(x, y) for o in runs for x, y in zip(o, w))
