@@ -435,7 +435,9 @@ nt_status nt_sdpa_paged_tree(const void *q, const nt_tensor_desc *dq, const nt_p
  *     m = max(m - w(x), 0) and w(x) = 0.
  *   Where no child stands, or the path is full, the next token is the first t with w(0) + .. + w(t) > last_uniform[b] * (the sum of w).  If w is 0 everywhere it is drawn
  *   from the node's target row so, and is -1 if that is 0 everywhere too.
- * Sums and comparisons are in 64 bits.  A draft outside the vocabulary is passed over, and so are a node's children behind its 64th.
+ * That makes the outcome one of the target's law where a node's children were drawn from its draft row each by itself (the same token may come twice).  Of children that are not, the
+ * likeliest or draws without putting back, the tokens that stand follow another law.  Without draft rows any children do: what is left of the target's row is exact.
+ * Sums, quotients and comparisons are in 64 bits.  A draft outside the vocabulary is passed over, and so are a node's children behind its 64th.
  * path (device int32 [sequences, room], unit stride along a row): the numbers of the tokens that stand, the root's 0 first, then -1;  accepted[b] (int32): how many,
  * the root with them (no new tokens: 0, and next[b] = -1);  next[b] (int64): the next token;  new_lengths[b] = lengths[b] - n + accepted[b] (both or neither may be NULL; they may
  * be one). */

@@ -782,7 +782,8 @@ def tree_masks(parents, starts, masks, depths, lengths=None, positions=None, win
 def verify_tree(target, draft, ids, parents, starts, uniform, last_uniform, path, accepted, next_ids, lengths=None, new_lengths=None, stream=None):
     """Which drafted tokens stand, and the token behind them: target and draft (or None) [tokens, vocabulary] probabilities behind each token, ids (int64) and parents
     of the tokens, random numbers uniform [tokens] and last_uniform [sequences] (float32).  Gives path [sequences, room], accepted [sequences], next_ids (int64
-    [sequences]) and, from lengths with all new tokens, new_lengths with those that stand.  See nt_verify_tree."""
+    [sequences]) and, from lengths with all new tokens, new_lengths with those that stand.  The outcome has the target's law where a node's children were drawn each by
+    itself from its draft row, or draft is None.  See nt_verify_tree."""
     if _recorder is None:
         st = (_calls or _load_calls()).verify_tree(target, draft, ids, parents, starts, uniform, last_uniform, path, accepted, next_ids, lengths, new_lengths, stream)
         if st is not None:

@@ -3,7 +3,8 @@
 // A sequence's new tokens are a tree, each token behind its parent: parents[t] is the parent's number within the sequence, -1 for none.
 //
 // Masks.  A token's mask has the bits of itself and its ancestors, its depth is their number less one.  A thread walks up from its token, with the parents in LDS; a word of
-// the mask is written when the walk, whose numbers fall, leaves it.  A launch, a load, LDS: 1.9 us for a chain of 8, 3.2 for 128 trees of 100.
+// the mask is written when the walk, whose numbers fall, leaves it.  A launch, a load, LDS: 1.9 us for a chain of 8, 3.2 for 128 trees of 100.  Bound
+// by the longest walk, a chain of reads: 128 chains of 100 13.8 us, one of 2000 1260, of 8000, whose parents are read from memory, 25 ms.
 //
 // Verification.  With p the target's row at a node, q the draft's, u and r given random numbers in [0, 1): w = p, m = 1; for each child in order, x its token,
 //   stands if u q(x) m < w(x)  (the walk goes on from there);  if not,  w = max(w / m - q, 0),  m = sum w.
@@ -13,7 +14,7 @@
 //
 // What has to be read are a few numbers of each draft, and the rows p and q of the node where the walk ends (and of those where more than one child is tried, for m).  One unit reads
 // 128000 words of both in 20 us, the chip 64 of them in 14: the rows are summed in chunks by all of it, then the chunk is searched in which the sum passes its goal.
-// Measured: 64 trees of 24 drafts, 128000 words fp32 64 to 90 us (walks meet two or three such nodes, in the longest five or more: what is behind the rounds is one unit's work; 21 us of sums, the chain of launches and loads the rest), one chain of 6, 32000
+// Measured: 64 trees of 24 drafts, 128000 words fp32 61 to 131 us, by the random numbers (walks meet two or three such nodes, in the longest five or more: what is behind the rounds is one unit's work; in a call of 85 40 us of sums, the chain of launches and loads the rest), one chain of 6, 32000
 // words, 11.4 us: walk 3.1, sums 1.9, search 4.8 us, each a chain of loads.
 #include <algorithm>
 #include <type_traits>
@@ -595,8 +596,8 @@ static nt_status launch_verify_kind(VerifyArgs &a, int64_t sequences, hipStream_
     const int64_t least = 256 * N, wanted = std::max<int64_t>(1, std::min<int64_t>(kMostChunks, 2048 / sequences));
     const int64_t chunk = std::max(least, ((a.V + wanted - 1) / wanted + least - 1) / least * least), chunks = (a.V + chunk - 1) / chunk;
     // A unit reads some 40 GB/s: of rows of 64 KB (both) and less one has enough (1 sequence, 8000 words 10.3 us, 10.8 in three launches; 32000 15.1, 11.4; 128000 30.9, 11.3).  Rounds
-    // before the last, whose sums are a unit's own work, are 3 us each where no walk needs one: only for long rows of trees that are likely to (us, 64 trees of 24, 128000 words: no round 98,
-    // four 64, six 77; 64000 71, 58; 32000 47, 53; chains of 6, 128000: 11.3, 13.7 with one).
+    // before the last, whose sums are a unit's own work, are 3 us each where no walk needs one: only for long rows of trees that are likely to (us, means of ten sets of random numbers, 64 trees of 24, 128000 words: no round 137,
+    // four 80, 131 at most, six 78, 89 at most; 64000 88, 67 with four; 32000 49, 51; chains of 6, 128000: 13.8, 18.0 with one).
     const int64_t row_bytes = (int64_t)a.V * (int64_t)sizeof(T) * (DRAFT ? 2 : 1);
     const int rounds = DRAFT && row_bytes > (256 << 10) ? (int)std::min<int64_t>(4, std::max<int64_t>(0, (a.T / sequences - 3) / 5)) : 0;
     WorkspaceLease lease;
