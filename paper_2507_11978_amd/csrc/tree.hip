@@ -596,7 +596,7 @@ static nt_status launch_verify_kind(VerifyArgs &a, int64_t sequences, hipStream_
     const int64_t least = 256 * N, wanted = std::max<int64_t>(1, std::min<int64_t>(kMostChunks, 2048 / sequences));
     const int64_t chunk = std::max(least, ((a.V + wanted - 1) / wanted + least - 1) / least * least), chunks = (a.V + chunk - 1) / chunk;
     // A unit reads some 40 GB/s: of rows of 64 KB (both) and less one has enough (1 sequence, 8000 words 10.3 us, 10.8 in three launches; 32000 15.1, 11.4; 128000 30.9, 11.3).  Rounds
-    // before the last, whose sums are a unit's own work, are 3 us each where no walk needs one: only for long rows of trees that are likely to (us, means of ten sets of random numbers, 64 trees of 24, 128000 words: no round 137,
+    // before the last, whose sums are a unit's own work, are 3 us each where no walk needs one: only for long rows of trees that are likely to (us, means of ten sets of random numbers, 64 trees of 24, 128000 words: none 137,
     // four 80, 131 at most, six 78, 89 at most; 64000 88, 67 with four; 32000 49, 51; chains of 6, 128000: 13.8, 18.0 with one).
     const int64_t row_bytes = (int64_t)a.V * (int64_t)sizeof(T) * (DRAFT ? 2 : 1);
     const int rounds = DRAFT && row_bytes > (256 << 10) ? (int)std::min<int64_t>(4, std::max<int64_t>(0, (a.T / sequences - 3) / 5)) : 0;
